@@ -88,6 +88,9 @@ typedef enum {
 #define TQ_DATA_BAD_PAD 8u      /* a nonzero pad digit (tail byte) or pad byte   */
 #define TQ_DATA_BAD_ROWPTR 16u  /* rowptr disagrees with the salience map        */
 #define TQ_DATA_BAD_WEIGHT 32u  /* tq_ternarize: an input weight is inf or NaN    */
+#define TQ_DATA_NO_PAGES 64u    /* tq_kv4_extend: more pages needed than are free  */
+#define TQ_DATA_BAD_SLOT 128u   /* tq_kv4_*: a slot, page, place or token range out
+                                   of bounds, or listed twice                     */
 
 /* A packed projection.  All pointers: device memory owned by the caller. */
 typedef struct {
@@ -497,6 +500,187 @@ TQ_API tq_status tq_ew_linear_batched(int32_t M, int32_t count, const tq_ew_prob
 #define TQ_STATIC_SCRATCH_BYTES ((size_t)1 << 20)
 TQ_API tq_status tq_linear_static(int32_t M, int32_t N, int32_t K, const tq_weight *w, const uint16_t *x,
                                   uint16_t *y, void *stream);
+
+/* ---------------------------------------------------------------------
+ * A K/V cache held in 4 bits, in pages (no counterpart in the paper, which
+ * leaves the cache in fp16; it is what a decode step reads beside the packed
+ * projections).
+ *
+ * Format.  A page holds TQ_KV_PAGE tokens.  In each layer a page has one
+ * block per K/V head, tq_kv4_block_bytes(dim) bytes:
+ *   K codes  [64][dim / 2]        dimension 2 b in the low half of byte b
+ *   V codes  [64][dim / 2]
+ *   K params [dim / 64][64] u16   one per group of 64 dimensions and token
+ *   V params [dim / 64][64] u16
+ * A param is an fp16 scale s of seven significant bits whose four low bits
+ * hold the zero z; the code c stands for s (c - z).  Four bits times seven
+ * bits are at most eleven: every value a cache holds is an fp16 number.
+ * Encoding of a group x (float32, IEEE operations):
+ *   lo = min(0, min x), hi = max(0, max x), s = fp16((hi - lo) / 15) rounded
+ *   up to a multiple of 16 of its units in the last place,
+ *   z = clamp(rint(-lo / s), 0, 15), c = clamp(rint(x / s) + z, 0, 15)
+ * (all zero where s = 0).  A group with a value that is not finite, or one
+ * whose values fp16 cannot hold (s max(z, 15 - z) > 65504), stands for NaN.
+ *
+ * Sequences.  A sequence is a slot: length[slot] tokens, token t in page
+ * table[slot][t / 64] at offset t % 64.  refs[page] counts the sequences that
+ * hold a page; a page with refs 0 is free.  A new cache has length and refs 0
+ * (table and data may hold anything).  Table entries beyond a sequence's
+ * pages are not read.  All state is device memory and every call is
+ * asynchronous: a step can be captured in a graph and grows no host state.
+ *
+ * Errors in device data (a slot or page out of range, a list that names a
+ * slot twice, too few free pages) are OR-ed into *d_status; nothing out of
+ * bounds is read or written. */
+#define TQ_KV_PAGE 64  /* tokens per page          */
+#define TQ_KV_GROUP 64 /* dimensions per scale     */
+typedef enum { TQ_F16 = 0, TQ_BF16 = 1 } tq_dtype;
+
+typedef struct {
+  int32_t layers, pages, heads; /* K/V heads; pages <= 2^24                    */
+  int32_t dim;                  /* 64 or 128                                   */
+  int32_t slots, max_pages;     /* sequences, and table entries of each        */
+  uint8_t *data;                /* [layers][pages][heads][block], 16-byte aligned */
+  int32_t *table;               /* [slots][max_pages]                          */
+  int32_t *length;              /* [slots]                                     */
+  int32_t *refs;                /* [pages]                                     */
+} tq_kv4_cache;
+
+/* Bytes of a block; 0 if dim is neither 64 nor 128. */
+TQ_API size_t tq_kv4_block_bytes(int32_t dim);
+
+/* Sequence upkeep.  `count` is the length of the (device) lists.
+ *
+ * tq_kv4_extend makes room for counts[i] >= 0 new tokens at the end of
+ * sequence slots[i], before they are written (tq_kv4_append) and attended to:
+ * length grows, new pages (refs 1) enter the table.  Where the new tokens
+ * begin inside a page that other sequences hold too, that page is first
+ * copied in every layer (copy on write).  Pages are the free ones in
+ * increasing order, given out in the order of the list, a copied page before
+ * the sequence's others; a page is free if refs was 0 when the call began.
+ *   tokens: host, the sum of counts (the places that `where` has room for);
+ *   indptr: out [count + 1], prefix sums of counts;
+ *   where: out [tokens], place page * 64 + offset of every new token.
+ * All or nothing: with too few free pages (TQ_DATA_NO_PAGES), a bad or
+ * repeated slot, a length past the table, or counts that do not add up to
+ * `tokens` (TQ_DATA_BAD_SLOT) no sequence changes, indptr is 0 and where -1.
+ *
+ * tq_kv4_fork gives the empty sequences dst[i] the contents of src[i]: they
+ * share its pages (refs grow; nothing is copied).  A pair whose slots are out
+ * of range, whose dst is not empty, or whose dst is listed again among the
+ * dst or src is left out (TQ_DATA_BAD_SLOT), as is one whose src is a dst.
+ *
+ * tq_kv4_free cuts sequence slots[i] to its first keep[i] tokens (0 where
+ * keep is NULL; a keep beyond the length changes nothing): refs of the pages
+ * past them fall, their table entries become -1.  Every copy of a slot listed
+ * twice is left out (TQ_DATA_BAD_SLOT).
+ *
+ * Callers order these calls on one stream (or by events) like any writes. */
+TQ_API size_t tq_kv4_extend_workspace_bytes(const tq_kv4_cache *c, int32_t count, int32_t tokens);
+TQ_API tq_status tq_kv4_extend(const tq_kv4_cache *c, int32_t count, const int32_t *slots, const int32_t *counts,
+                               int32_t tokens, int32_t *indptr, int32_t *where, void *workspace,
+                               size_t workspace_bytes, uint32_t *d_status, void *stream);
+TQ_API tq_status tq_kv4_fork(const tq_kv4_cache *c, int32_t count, const int32_t *src, const int32_t *dst,
+                             uint32_t *d_status, void *stream);
+TQ_API tq_status tq_kv4_free(const tq_kv4_cache *c, int32_t count, const int32_t *slots, const int32_t *keep,
+                             uint32_t *d_status, void *stream);
+
+/* Moves the pages in use to the front of the pool: with n pages in use, the
+ * i-th free page below n receives the contents (every layer) of the i-th used
+ * page from n on.  table_out / refs_out: the state after the move (they may be
+ * the cache's own arrays); remap: out [pages], the new page of every used one,
+ * -1 for free ones; live: out [1], n.  The cache's arrays are otherwise only
+ * read; entries of table_out past a sequence's pages are -1. */
+TQ_API size_t tq_kv4_compact_workspace_bytes(const tq_kv4_cache *c);
+TQ_API tq_status tq_kv4_compact(const tq_kv4_cache *c, int32_t *table_out, int32_t *refs_out, int32_t *remap,
+                                int32_t *live, void *workspace, size_t workspace_bytes, uint32_t *d_status,
+                                void *stream);
+/* Copies page src_pages[i] of cache `from` to page dst_pages[i] of cache `to`
+ * in every layer (bytes only; refs and tables are the caller's).  The caches
+ * agree in layers, heads and dim and may be the same; no destination may be
+ * among the sources or twice among the destinations.  Pairs out of range are
+ * left out (TQ_DATA_BAD_SLOT). */
+TQ_API tq_status tq_kv4_copy_pages(const tq_kv4_cache *from, const tq_kv4_cache *to, int32_t count,
+                                   const int32_t *src_pages, const int32_t *dst_pages, uint32_t *d_status,
+                                   void *stream);
+
+/* Encodes the keys and values of `tokens` tokens into one layer at the places
+ * where[] (tq_kv4_extend; a negative place is skipped, one beyond the pool is
+ * skipped and reported; no place may be listed twice).
+ *   k, v: [tokens][heads][dim], token t's row from element t * stride on (so
+ *   columns of a fused projection's output can be passed); dtype TQ_F16 or
+ *   TQ_BF16; strides >= heads * dim. */
+TQ_API tq_status tq_kv4_append(const tq_kv4_cache *c, int32_t layer, int32_t tokens, int32_t dtype, const uint16_t *k,
+                               int64_t k_stride, const uint16_t *v, int64_t v_stride, const int32_t *where,
+                               uint32_t *d_status, void *stream);
+/* The values held at the places where[]: k, v out [tokens][heads][dim] (fp16
+ * exactly, bf16 rounded to nearest even; zeros for a skipped place). */
+TQ_API tq_status tq_kv4_read(const tq_kv4_cache *c, int32_t layer, int32_t tokens, int32_t dtype, const int32_t *where,
+                             uint16_t *k, uint16_t *v, uint32_t *d_status, void *stream);
+
+/* Attention over one layer of the cache.  Queries of sequence slots[b] are
+ * the tokens indptr[b] .. indptr[b + 1] - 1 of q, its last ones: token i of n
+ * stands at position length - n + i.  Query head h reads K/V head
+ * h / (q_heads / heads).
+ *   out[t][h] = sum_j p_j v_j,  p = softmax_j(scale * q . k_j)
+ * over the positions j of its sequence that the token sees: j <= its own
+ * (causal != 0) and, with window > 0, j > its own - window; all of them with
+ * causal = 0 (window must then be 0).  A token that sees nothing (a position
+ * below 0) gets zeros and lse -inf.  Products and sums are fp32; p is
+ * rounded to fp16 (with the rounding's rest carried along where there are few
+ * query rows) for its product with the values.
+ *   q: [tokens][q_heads][dim], token t's row from element t * q_stride on
+ *   (a multiple of 8), 16-byte aligned; out the same with out_stride; lse:
+ *   optional fp32 [tokens][q_heads], the natural logarithm of the sum;
+ *   max_q: an upper bound of a sequence's tokens in this call (at most
+ *   `tokens`; it chooses kernels, a bound that is too small costs time and not
+ *   results); q_heads a multiple of heads;
+ *   workspace: tq_kv4_attention_workspace_bytes bytes, 256-byte aligned.
+ * Sequences with a bad slot, range or page are reported (TQ_DATA_BAD_SLOT);
+ * their outputs are unspecified.  Tokens outside every range are not written. */
+TQ_API size_t tq_kv4_attention_workspace_bytes(const tq_kv4_cache *c, int32_t count, int32_t tokens, int32_t max_q,
+                                               int32_t q_heads);
+TQ_API tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t count, const int32_t *slots,
+                                  const int32_t *indptr, int32_t tokens, int32_t max_q, int32_t q_heads, int32_t dtype,
+                                  const uint16_t *q, int64_t q_stride, float scale, int32_t causal, int32_t window,
+                                  uint16_t *out, int64_t out_stride, float *lse, void *workspace,
+                                  size_t workspace_bytes, uint32_t *d_status, void *stream);
+
+/* ---------------------------------------------------------------------
+ * 4-bit weights with group scales, for the projections that are not ternary
+ * (the output head above all; the paper leaves them in fp16):
+ *   W[n][k] = scale[n][g] * c[n][k] + minimum[n][g],  g = k / 128, c in 0..15
+ * with fp16 scale and minimum (symmetric and zero-point schemes are special
+ * cases).  `tiles` holds, for every 16 rows and then every group, 1088 bytes:
+ * the codes [16][64] (column 2 b of the group in the low half of byte b), then
+ * (scale, minimum) [16]; rows past N are zeros. */
+typedef struct {
+  int32_t N, K;         /* K a multiple of 128 */
+  const uint8_t *tiles; /* 16-byte aligned, tq_w4_bytes(N, K) bytes */
+} tq_w4_weight;
+TQ_API size_t tq_w4_bytes(int32_t N, int32_t K);
+/* From codes uint8 [N][K] (above 15: TQ_DATA_BAD_CODE, the low four bits are
+ * kept) and fp16 scale, minimum [N][K / 128]. */
+TQ_API tq_status tq_w4_pack(int32_t N, int32_t K, const uint8_t *codes, const uint16_t *scale, const uint16_t *minimum,
+                            uint8_t *tiles, uint32_t *d_status, void *stream);
+/* Round-to-nearest quantization of fp16 W [N][K] (16-byte aligned), per group:
+ * minimum = min w, scale = fp16((max w - minimum) / 15),
+ * c = clamp(rint((w - minimum) / scale), 0, 15) in float32 (0 where scale is
+ * 0).  A weight that is not finite sets TQ_DATA_BAD_WEIGHT; its group then
+ * stands for NaN. */
+TQ_API tq_status tq_w4_quantize(int32_t N, int32_t K, const uint16_t *W, uint8_t *tiles, uint32_t *d_status,
+                                void *stream);
+/* W as dense fp16 [N][K] (16-byte aligned; one rounding). */
+TQ_API tq_status tq_w4_dequantize(int32_t N, int32_t K, const tq_w4_weight *w, uint16_t *out, void *stream);
+/* y = x W^T: x fp16 [M][K] (16-byte aligned), y fp16 [M][N] (tq_w4_linear_f32out:
+ * fp32).  M >= 1.  The codes are multiplied as they are and the scales and
+ * minima applied in fp32, so no weight is rounded.  Workspace:
+ * tq_w4_workspace_bytes(M, N, K) bytes, 256-byte aligned, overwritten. */
+TQ_API size_t tq_w4_workspace_bytes(int32_t M, int32_t N, int32_t K);
+TQ_API tq_status tq_w4_linear(int32_t M, int32_t N, int32_t K, const tq_w4_weight *w, const uint16_t *x, uint16_t *y,
+                              void *workspace, size_t workspace_bytes, void *stream);
+TQ_API tq_status tq_w4_linear_f32out(int32_t M, int32_t N, int32_t K, const tq_w4_weight *w, const uint16_t *x,
+                                     float *y, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Device status word of the library's linear kernels, OR of:
  *   1 = a bounded device-side wait ran out (the kernel stopped early and its

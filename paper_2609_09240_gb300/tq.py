@@ -60,6 +60,16 @@ class tq_ew_problem(ctypes.Structure):
     _fields_ = [("w", tq_ew_weight), ("x", ctypes.c_void_p), ("y", ctypes.c_void_p)]
 
 
+class tq_kv4_cache(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("slots", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("data", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("length", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class tq_w4_weight(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("tiles", ctypes.c_void_p)]
+
+
 class tq_host_weight(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("nnz", ctypes.c_int64),
                 ("plane1", ctypes.c_void_p), ("salience", ctypes.c_void_p), ("rowptr", ctypes.c_void_p),
@@ -160,6 +170,30 @@ def lib():
             L.tq_container_check_keys.restype = ctypes.c_int
             L.tq_container_check_keys.argtypes = [vp, sz, i32, ctypes.POINTER(ctypes.c_char_p),
                                                   ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
+            KV, W4, f32 = ctypes.POINTER(tq_kv4_cache), ctypes.POINTER(tq_w4_weight), ctypes.c_float
+            for name, res, args in (
+                    ("tq_kv4_block_bytes", sz, [i32]),
+                    ("tq_kv4_extend_workspace_bytes", sz, [KV, i32, i32]),
+                    ("tq_kv4_extend", ctypes.c_int, [KV, i32, vp, vp, i32, vp, vp, vp, sz, vp, vp]),
+                    ("tq_kv4_fork", ctypes.c_int, [KV, i32, vp, vp, vp, vp]),
+                    ("tq_kv4_free", ctypes.c_int, [KV, i32, vp, vp, vp, vp]),
+                    ("tq_kv4_compact_workspace_bytes", sz, [KV]),
+                    ("tq_kv4_compact", ctypes.c_int, [KV, vp, vp, vp, vp, vp, sz, vp, vp]),
+                    ("tq_kv4_copy_pages", ctypes.c_int, [KV, KV, i32, vp, vp, vp, vp]),
+                    ("tq_kv4_append", ctypes.c_int, [KV, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp]),
+                    ("tq_kv4_read", ctypes.c_int, [KV, i32, i32, i32, vp, vp, vp, vp, vp]),
+                    ("tq_kv4_attention_workspace_bytes", sz, [KV, i32, i32, i32, i32]),
+                    ("tq_kv4_attention", ctypes.c_int, [KV, i32, i32, vp, vp, i32, i32, i32, i32, vp, i64, f32, i32, i32,
+                                                        vp, i64, vp, vp, sz, vp, vp]),
+                    ("tq_w4_bytes", sz, [i32, i32]),
+                    ("tq_w4_pack", ctypes.c_int, [i32, i32, vp, vp, vp, vp, vp, vp]),
+                    ("tq_w4_quantize", ctypes.c_int, [i32, i32, vp, vp, vp, vp]),
+                    ("tq_w4_dequantize", ctypes.c_int, [i32, i32, W4, vp, vp]),
+                    ("tq_w4_workspace_bytes", sz, [i32, i32, i32]),
+                    ("tq_w4_linear", ctypes.c_int, [i32, i32, i32, W4, vp, vp, vp, sz, vp]),
+                    ("tq_w4_linear_f32out", ctypes.c_int, [i32, i32, i32, W4, vp, vp, vp, sz, vp])):
+                fn = getattr(L, name)
+                fn.restype, fn.argtypes = res, args
             L.tq_wait_selftest.restype = ctypes.c_int
             L.tq_wait_selftest.argtypes = [vp, vp]
             L.tq_get_device_status.restype = ctypes.c_int
@@ -726,3 +760,289 @@ class EwBatch:
 def tq_ew_linear_batched(batch: EwBatch, stream=None):
     _check(lib().tq_ew_linear_batched(batch.M, len(batch.items), batch.arr, _p(batch.ws), batch.ws.numel(),
                                       _stream(stream)), "tq_ew_linear_batched")
+
+
+# ------------------------------------------------------- 4-bit K/V cache
+TQ_KV_PAGE, TQ_KV_GROUP = 64, 64
+DATA_NO_PAGES, DATA_BAD_SLOT = 64, 128
+_KV_DTYPE = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def _want(t, name, dtype, shape=None):
+    """A contiguous CUDA tensor of the given type (and shape); its pointer."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _p(t)
+
+
+def _rows(t, name, heads, dim):
+    """(pointer, elements between tokens) of a [tokens][heads][dim] tensor whose
+    heads lie side by side; tokens may be any distance apart."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("expected a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor (device memory)")
+    if t.dtype not in _KV_DTYPE:
+        raise ValueError(f"{name}: expected fp16 or bf16, got {t.dtype}")
+    T = t.shape[0]
+    if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name}: expected [tokens][{heads or 'heads'}][{dim}], got {tuple(t.shape)}")
+    if T and ((t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != dim)):
+        raise ValueError(f"{name}: the heads of a token must lie side by side")
+    row = t.shape[1] * dim
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if T > 1 else row)
+
+
+class Kv4Cache:
+    """A 4-bit K/V cache (tq_kv4_cache): device tensors, a status word that the
+    calls OR data errors into, and their scratch memory (one per stream).
+
+    data uint8 [layers][pages][heads][block], table int32 [slots][max_pages],
+    length int32 [slots], refs int32 [pages]."""
+
+    def __init__(self, data, table, length, refs, dim):
+        layers, pages, heads, block = data.shape
+        if block != int(lib().tq_kv4_block_bytes(dim)):
+            raise TQError(-2, "tq_kv4_block_bytes")
+        slots, max_pages = table.shape
+        self.data, self.table, self.length, self.refs, self.dim = data, table, length, refs, dim
+        self.layers, self.pages, self.heads, self.slots, self.max_pages = layers, pages, heads, slots, max_pages
+        self.status = torch.zeros(1, dtype=torch.int32, device=data.device)
+        c = tq_kv4_cache(layers, pages, heads, dim, slots, max_pages)
+        c.data, c.table = _want(data, "data", torch.uint8), _want(table, "table", torch.int32)
+        c.length, c.refs = (_want(length, "length", torch.int32, (slots,)), _want(refs, "refs", torch.int32, (pages,)))
+        self._struct, self._ref = c, ctypes.byref(c)
+        self._ws, self._outgrown, self._sizes = {}, [], {}
+
+    @classmethod
+    def empty(cls, layers, pages, heads, dim, slots, max_pages, device="cuda"):
+        """A new cache without sequences."""
+        i32 = dict(dtype=torch.int32, device=device)
+        block = int(lib().tq_kv4_block_bytes(dim))
+        if block == 0:
+            raise TQError(-2, "tq_kv4_block_bytes")
+        return cls(torch.empty((layers, pages, heads, block), dtype=torch.uint8, device=device),
+                   torch.full((slots, max_pages), -1, **i32), torch.zeros(slots, **i32), torch.zeros(pages, **i32), dim)
+
+    def _scratch(self, stream, fn, *args):
+        """The stream's scratch memory, at least as large as `fn`(cache, *args)
+        says.  One that was outgrown is kept (work in flight may use it); sizes
+        double, so all of them together are no more than twice the largest."""
+        key = (fn, args)
+        n = self._sizes.get(key)
+        if n is None:
+            n = int(getattr(lib(), fn)(self._ref, *args))
+            if n == 0:
+                raise TQError(-2, fn)
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            self._sizes[key] = n
+        ws = self._ws.get(stream.value)
+        if ws is None or ws.numel() < n:
+            if ws is not None:
+                self._outgrown.append(ws)
+                n = max(n, 2 * ws.numel())
+            ws = self._ws[stream.value] = workspace(n, self.data.device)
+        return ctypes.c_void_p(ws.data_ptr()), ws.numel()
+
+    def check(self):
+        """Raise on data errors that earlier calls reported (synchronizes; clears them)."""
+        st = int(self.status.item())
+        if st:
+            self.status.zero_()
+            raise TQError(-4, f"4-bit cache: data status {st:#x}")
+
+
+def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, where=None, stream=None):
+    """Room for counts[i] new tokens at the end of sequences slots[i] (int32
+    device lists; tokens: their sum).  Returns (indptr [count + 1], where
+    [tokens]), the token ranges for tq_kv4_attention and the places for
+    tq_kv4_append."""
+    n = slots.shape[0]
+    if indptr is None:
+        indptr = torch.empty(n + 1, dtype=torch.int32, device=slots.device)
+    if where is None:
+        where = torch.empty(tokens, dtype=torch.int32, device=slots.device)
+    st = _stream(stream)
+    ws, nws = cache._scratch(st, "tq_kv4_extend_workspace_bytes", n, tokens)
+    i32 = torch.int32
+    _check(lib().tq_kv4_extend(cache._ref, n, _want(slots, "slots", i32, (n,)), _want(counts, "counts", i32, (n,)),
+                               tokens, _want(indptr, "indptr", i32, (n + 1,)), _want(where, "where", i32, (tokens,)), ws,
+                               nws, _p(cache.status), st), "tq_kv4_extend")
+    return indptr, where
+
+
+def tq_kv4_fork(cache: Kv4Cache, src, dst, stream=None):
+    """Empty sequences dst[i] become copies of sequences src[i] that share their pages."""
+    n = src.shape[0]
+    _check(lib().tq_kv4_fork(cache._ref, n, _want(src, "src", torch.int32, (n,)), _want(dst, "dst", torch.int32, (n,)),
+                             _p(cache.status), _stream(stream)), "tq_kv4_fork")
+
+
+def tq_kv4_free(cache: Kv4Cache, slots, keep=None, stream=None):
+    """Sequences slots[i] cut to keep[i] tokens (0 without keep)."""
+    n = slots.shape[0]
+    k = None if keep is None else _want(keep, "keep", torch.int32, (n,))
+    _check(lib().tq_kv4_free(cache._ref, n, _want(slots, "slots", torch.int32, (n,)), k, _p(cache.status),
+                             _stream(stream)), "tq_kv4_free")
+
+
+def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, live=None, stream=None):
+    """The pages in use moved to the front of the pool; table and refs change
+    in place unless table_out / refs_out are given.  Returns (remap [pages],
+    live [1])."""
+    i32 = dict(dtype=torch.int32, device=cache.data.device)
+    table_out = cache.table if table_out is None else table_out
+    refs_out = cache.refs if refs_out is None else refs_out
+    remap = torch.empty(cache.pages, **i32) if remap is None else remap
+    live = torch.empty(1, **i32) if live is None else live
+    st = _stream(stream)
+    ws, nws = cache._scratch(st, "tq_kv4_compact_workspace_bytes")
+    _check(lib().tq_kv4_compact(cache._ref, _want(table_out, "table_out", torch.int32, cache.table.shape),
+                                _want(refs_out, "refs_out", torch.int32, cache.refs.shape),
+                                _want(remap, "remap", torch.int32, (cache.pages,)),
+                                _want(live, "live", torch.int32, (1,)), ws, nws, _p(cache.status), st),
+           "tq_kv4_compact")
+    return remap, live
+
+
+def tq_kv4_copy_pages(src: Kv4Cache, dst: Kv4Cache, src_pages, dst_pages, stream=None):
+    """Page src_pages[i] of cache src, every layer, into page dst_pages[i] of cache dst."""
+    n = src_pages.shape[0]
+    _check(lib().tq_kv4_copy_pages(src._ref, dst._ref, n, _want(src_pages, "src_pages", torch.int32, (n,)),
+                                   _want(dst_pages, "dst_pages", torch.int32, (n,)), _p(dst.status), _stream(stream)),
+           "tq_kv4_copy_pages")
+
+
+def tq_kv4_append(k, v, cache: Kv4Cache, layer: int, where, stream=None):
+    """Keys and values [tokens][heads][dim] (fp16 or bf16; the heads of a token
+    side by side, tokens any distance apart) into the places where[]."""
+    kp, ks = _rows(k, "k", cache.heads, cache.dim)
+    vp, vs = _rows(v, "v", cache.heads, cache.dim)
+    T = k.shape[0]
+    if v.shape[0] != T or v.dtype != k.dtype:
+        raise ValueError("k and v differ in tokens or type")
+    _check(lib().tq_kv4_append(cache._ref, layer, T, _KV_DTYPE[k.dtype], kp, ks, vp, vs,
+                               _want(where, "where", torch.int32, (T,)), _p(cache.status), _stream(stream)),
+           "tq_kv4_append")
+
+
+def tq_kv4_read(cache: Kv4Cache, layer: int, where, dtype=torch.float16, k=None, v=None, stream=None):
+    """The keys and values held at the places where[]: two [tokens][heads][dim] tensors."""
+    T = where.shape[0]
+    shape = (T, cache.heads, cache.dim)
+    k = torch.empty(shape, dtype=dtype, device=where.device) if k is None else k
+    v = torch.empty(shape, dtype=dtype, device=where.device) if v is None else v
+    if dtype not in _KV_DTYPE:
+        raise ValueError(f"expected fp16 or bf16, got {dtype}")
+    _check(lib().tq_kv4_read(cache._ref, layer, T, _KV_DTYPE[dtype], _want(where, "where", torch.int32, (T,)),
+                             _want(k, "k", dtype, shape), _want(v, "v", dtype, shape), _p(cache.status),
+                             _stream(stream)), "tq_kv4_read")
+    return k, v
+
+
+def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, scale=None, causal=True, window=0,
+                     out=None, lse=None, stream=None):
+    """Attention of q [tokens][q_heads][dim] (fp16 or bf16) over one layer of
+    the cache; sequence slots[b] has the queries indptr[b] .. indptr[b + 1] - 1,
+    its last tokens.  max_q: the most queries of a sequence, if known (1 in a
+    decode step).  scale: 1 / sqrt(dim) if None.  lse: optional fp32
+    [tokens][q_heads] output.  Returns out."""
+    qp, qs = _rows(q, "q", None, cache.dim)
+    T, Hq = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty((T, Hq, cache.dim), dtype=q.dtype, device=q.device)
+    op, os_ = _rows(out, "out", Hq, cache.dim)
+    if out.dtype != q.dtype or out.shape[0] != T:
+        raise ValueError("out and q differ in tokens or type")
+    n = slots.shape[0]
+    max_q = T if max_q is None else min(int(max_q), T)
+    st = _stream(stream)
+    ws, nws = cache._scratch(st, "tq_kv4_attention_workspace_bytes", n, T, max_q, Hq)
+    lp = None if lse is None else _want(lse, "lse", torch.float32, (T, Hq))
+    _check(lib().tq_kv4_attention(cache._ref, layer, n, _want(slots, "slots", torch.int32, (n,)),
+                                  _want(indptr, "indptr", torch.int32, (n + 1,)), T, max_q, Hq, _KV_DTYPE[q.dtype], qp,
+                                  qs, cache.dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
+                                  int(window), op, os_, lp, ws, nws, _p(cache.status), st), "tq_kv4_attention")
+    return out
+
+
+# ------------------------------------------------- 4-bit weights with scales
+class W4Weight:
+    """A projection in 4 bits (tq_w4_weight): its tiles on the device."""
+
+    def __init__(self, N, K, tiles):
+        self.N, self.K, self.tiles = N, K, tiles
+        s = tq_w4_weight(N, K)
+        s.tiles = tiles.data_ptr()
+        self._struct, self._ref = s, ctypes.byref(s)
+
+    @classmethod
+    def _new(cls, N, K, device):
+        n = int(lib().tq_w4_bytes(N, K))
+        if n == 0:
+            raise TQError(-2, "tq_w4_bytes")
+        return cls(N, K, torch.empty(n, dtype=torch.uint8, device=device))
+
+    def packed_bytes(self) -> int:
+        return self.tiles.numel()
+
+
+def _w4_made(call, where, dev, check):
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    _check(call(_p(status)), where)
+    if check:
+        st = int(status.item())
+        if st:
+            raise TQError(-4, f"{where} data status {st:#x}")
+
+
+def pack_w4(codes, scale, minimum, stream=None, check=True) -> W4Weight:
+    """uint8 codes [N][K] (0 .. 15), fp16 scale and minimum [N][K / 128] ->
+    W4Weight.  check reads the data status back (one synchronization)."""
+    N, K = codes.shape
+    w = W4Weight._new(N, K, codes.device)
+    g = (N, K // TQ_GROUP)
+    cp, sp, mp = (_want(codes, "codes", torch.uint8), _want(scale, "scale", torch.float16, g),
+                  _want(minimum, "minimum", torch.float16, g))
+    _w4_made(lambda st: lib().tq_w4_pack(N, K, cp, sp, mp, _p(w.tiles), st, _stream(stream)), "tq_w4_pack",
+             codes.device, check)
+    return w
+
+
+def quantize_w4(W, stream=None, check=True) -> W4Weight:
+    """Round-to-nearest 4-bit weights of fp16 W [N][K] on the device."""
+    N, K = W.shape
+    w = W4Weight._new(N, K, W.device)
+    wp = _want(W, "W", torch.float16)
+    _w4_made(lambda st: lib().tq_w4_quantize(N, K, wp, _p(w.tiles), st, _stream(stream)), "tq_w4_quantize", W.device,
+             check)
+    return w
+
+
+def tq_w4_dequantize(w: W4Weight, out=None, stream=None):
+    """W as dense fp16 [N][K] on the device."""
+    if out is None:
+        out = torch.empty((w.N, w.K), dtype=torch.float16, device=w.tiles.device)
+    _check(lib().tq_w4_dequantize(w.N, w.K, w._ref, _want(out, "out", torch.float16, (w.N, w.K)), _stream(stream)),
+           "tq_w4_dequantize")
+    return out
+
+
+def tq_w4_linear(x, w: W4Weight, y=None, ws=None, stream=None, f32=False):
+    """y = x W^T for 4-bit weights; x fp16 [M][K], y fp16 [M][N] (fp32 with f32=True)."""
+    M = x.shape[0]
+    dt = torch.float32 if f32 else torch.float16
+    xp = _want(x, "x", torch.float16, (M, w.K))
+    if y is None:
+        y = torch.empty((M, w.N), dtype=dt, device=x.device)
+    if ws is None:
+        n = int(lib().tq_w4_workspace_bytes(M, w.N, w.K))
+        if n == 0:
+            raise TQError(-2, "tq_w4_workspace_bytes")
+        ws = workspace(n, x.device)
+    fn = lib().tq_w4_linear_f32out if f32 else lib().tq_w4_linear
+    _check(fn(M, w.N, w.K, w._ref, xp, _want(y, "y", dt, (M, w.N)), _p(ws), ws.numel(), _stream(stream)), "tq_w4_linear")
+    return y
