@@ -48,6 +48,9 @@ cudaError_t launch_ternarize(int N, int K, const uint16_t *W, int64_t nnz, int s
 cudaError_t read_status_prefill(uint32_t *out, bool clear);
 cudaError_t read_status_selftest(uint32_t *out, bool clear);
 cudaError_t launch_wait_selftest(int32_t *result, cudaStream_t s);
+namespace kv4 {
+cudaError_t read_status_kv4_attention(uint32_t *out, bool clear);
+}
 }  // namespace tq
 
 using namespace tq;
@@ -621,12 +624,13 @@ tq_status tq_ew_linear_f32out(int32_t M, int32_t N, int32_t K, const tq_ew_weigh
 
 tq_status tq_get_device_status(uint32_t *status_host, int clear) {
   if (!status_host) return TQ_ERR_NULL;
-  uint32_t b = 0, c = 0, d = 0, e = 0;
+  uint32_t b = 0, c = 0, d = 0, e = 0, f = 0;
   if (read_status_gemv_mma(&b, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (read_status_gemv_g4(&e, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (read_status_prefill(&c, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (read_status_selftest(&d, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
-  *status_host = b | c | d | e;
+  if (kv4::read_status_kv4_attention(&f, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
+  *status_host = b | c | d | e | f;
   return TQ_OK;
 }
 

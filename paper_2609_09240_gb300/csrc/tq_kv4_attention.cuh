@@ -1,0 +1,33 @@
+// tq_kv4_attention.cuh - arguments of the attention kernels over the 4-bit K/V cache.
+#pragma once
+
+#include "tq_kv4.cuh"
+
+namespace tq {
+namespace kv4 {
+
+struct AttnArgs {
+  tq_kv4_cache c;
+  int32_t layer, count, tokens, q_heads, causal, window;
+  const int32_t *slots, *indptr;
+  const uint16_t *q;
+  uint16_t *out;
+  float *lse;
+  int64_t q_stride, out_stride;
+  float scale;
+  uint32_t *d_status;
+};
+
+// Two results in the output's type.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
+  uint32_t r;
+  if (BF16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+}  // namespace kv4
+}  // namespace tq
