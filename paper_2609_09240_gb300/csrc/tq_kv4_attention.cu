@@ -28,11 +28,10 @@
 // through its own ring of shared memory and keeps the softmax's running
 // maximum and sum; runs that end inside a sequence leave a partial result that
 // attn_combine_kernel joins.
-#include <math_constants.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <limits>
 
 #include "tq_kv4_attention.cuh"
 #include "tq_launch.cuh"
@@ -41,8 +40,16 @@
 namespace tq {
 namespace kv4 {
 
-constexpr int kSplitWarps = 8;
-constexpr int kSplitThreads = kSplitWarps * 32;
+// Warps of a block (one block per SM) for NT tiles of eight query rows, and the
+// blocks of 64 tokens that each has under way.  One tile leaves the registers
+// for twelve warps: 48 sequences of 1000 to 8000 tokens take 76 us with twelve
+// (two blocks each) and 80 with eight (three); two tiles spill with twelve, and
+// a few queries for each of 16 sequences take 18 us with eight and 21 with twelve.
+template <int D, int NT>
+struct Shape {
+  static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = kWarps * 32;
+  static constexpr int kStages = (NT == 1 ? 2 : 3) * (D == 128 ? 1 : 2);
+};
 constexpr int kMaxSeqs = 512;  // sequences of a launch
 
 // Sequences as the kernels see them, in shared memory.
@@ -59,12 +66,12 @@ __device__ __forceinline__ void seq_pages(const AttnArgs &a, int L, int n, int *
 }
 
 // Fills the table; every thread of the block calls it.  part: scratch.
-__device__ __forceinline__ void load_seqs(const AttnArgs &a, int rows_per_tile, SeqTable &T, int64_t *part,
-                                          bool tell) {
+template <int WARPS>
+__device__ __forceinline__ void load_seqs(const AttnArgs &a, int rows_per_tile, SeqTable &T, int64_t *part) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = a.q_heads / a.c.heads;
   int64_t carry = 0;
-  for (int base = 0; base < a.count; base += kSplitThreads) {
+  for (int base = 0; base < a.count; base += WARPS * 32) {
     const int b = base + tid;
     int64_t u = 0;
     if (b < a.count) {
@@ -75,7 +82,7 @@ __device__ __forceinline__ void load_seqs(const AttnArgs &a, int rows_per_tile, 
         L = a.c.length[slot];
         bad = L != clamp_length(a.c, L);
       }
-      if (bad && tell) report(a.d_status, TQ_DATA_BAD_SLOT);
+      if (bad && blockIdx.x == 0) report(a.d_status, TQ_DATA_BAD_SLOT);
       T.slot[b] = slot;
       T.q0[b] = q0;
       T.L[b] = L;
@@ -98,7 +105,7 @@ __device__ __forceinline__ void load_seqs(const AttnArgs &a, int rows_per_tile, 
     __syncthreads();
     int64_t before = carry, all = carry;
 #pragma unroll
-    for (int w = 0; w < kSplitWarps; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
       if (w < warp) before += part[w];
       all += part[w];
     }
@@ -121,17 +128,77 @@ __device__ __forceinline__ int find_seq(const SeqTable &T, int count, int64_t u)
   return lo;
 }
 
-// The first unit of worker w of W, and the worker that has unit u.
-__device__ __forceinline__ int64_t first_unit(int w, int W, int64_t U) { return U * w / W; }
-__device__ __forceinline__ int worker_of(int64_t u, int W, int64_t U) { return (int)(((u + 1) * W - 1) / U); }
+// Runs of units: the first `more` workers (warps, block by block) take each + 1,
+// the others `each`.
+struct Runs {
+  int64_t each;
+  int32_t more;
+  __device__ __forceinline__ Runs(int64_t U, int W) : each(U / W), more((int32_t)(U % W)) {}
+  __device__ __forceinline__ int64_t first(int w) const { return each * w + min(w, more); }
+  // the worker that has unit u
+  __device__ __forceinline__ int worker(int64_t u) const {
+    const int64_t head = (each + 1) * more;
+    return (int)(u < head ? u / (each + 1) : more + (u - head) / each);
+  }
+};
 
-// Partial results: worker w's piece of the segment that it begins with (slot 0)
-// and of the last one (slot 1): D values of each row, then the logarithms that
-// the values refer to, then the sums.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kInf = std::numeric_limits<float>::infinity();
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// A partial result: D values of each row, then the logarithms that the values
+// refer to, then the sums.  A warp leaves at most two, of the segment that its
+// run begins inside or with (slot 0) and of its last one (slot 1).  Where a
+// block's whole run lies inside one segment, its warps' parts become one (slot 0
+// of its first warp).
 template <int D, int NT>
 struct Part {
-  static constexpr int kRows = 8 * NT;
+  static constexpr int kRows = 8 * NT, kLanes = D / 4;  // a thread joins four dimensions of a row
   static constexpr int kFloats = kRows * (D + 2);
+};
+// What attn_combine_kernel joins, one per worker: the worker after the one that
+// begins a shared segment names its parts and its rows.
+struct alignas(16) Join {
+  int32_t w0, w1;  // the segment's workers; w1 < 0: nothing to join
+  int32_t slot0;   // where w0's part is (the others': slot 0)
+  int32_t f0, f1;  // blocks whose whole run is the segment's
+  int32_t row0, rows, q0, h;
+};
+
+// Part of the softmax over some of the keys, and how two become one.
+struct Soft {
+  float m, l;
+  float4 o;
+  __device__ __forceinline__ Soft() : m(-kInf), l(0.0f), o(make_float4(0, 0, 0, 0)) {}
+  __device__ __forceinline__ void join(float pm, float pl, const float4 &po) {
+    const float nm = fmaxf(m, pm), at = nm == -kInf ? 0.0f : nm;
+    const float fa = exp2_fast(m - at), fb = exp2_fast(pm - at);
+    l = l * fa + pl * fb;
+    o.x = o.x * fa + po.x * fb;
+    o.y = o.y * fa + po.y * fb;
+    o.z = o.z * fa + po.z * fb;
+    o.w = o.w * fa + po.w * fb;
+    m = nm;
+  }
+  template <int D, int NT>
+  __device__ __forceinline__ void join(const float *p, int r, int lane) {
+    join(p[Part<D, NT>::kRows * D + r], p[Part<D, NT>::kRows * (D + 1) + r],
+         reinterpret_cast<const float4 *>(p + r * D)[lane]);
+  }
+  template <int D, bool BF16>
+  __device__ __forceinline__ void write(const AttnArgs &a, int q0, int row, int h, int lane) const {
+    const int g = a.q_heads / a.c.heads;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t token = q0 + row / g;
+    const int head = h * g + row % g;
+    *reinterpret_cast<uint2 *>(a.out + token * a.out_stride + head * D + 4 * lane) =
+        make_uint2(pack_out<BF16>(o.x * inv, o.y * inv), pack_out<BF16>(o.z * inv, o.w * inv));
+    if (lane == 0 && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -kInf : kLn2 * (m + log2f(l));
+  }
 };
 
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
@@ -139,6 +206,13 @@ __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same onto zeros.
+__device__ __forceinline__ void mma_f16_first(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
@@ -150,43 +224,48 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+// (w & mask) | bits in one instruction: with two constants the compiler would
+// take two, it keeps no more than one immediate in an instruction.
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
 }
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
+// 1024 + (64 +) the nibble at bits 0 (4) of both 16-bit halves.
+__device__ __forceinline__ __half2 low_nibbles(uint32_t w) { return as_half2(and_or(w, 0x000F000Fu, 0x64006400u)); }
+__device__ __forceinline__ __half2 high_nibbles(uint32_t w) { return as_half2(and_or(w, 0x00F000F0u, 0x54005400u)); }
 // c - z of nibble I of both 16-bit halves; za = 1024 + z, zb = 64 + z.
 template <int I>
 __device__ __forceinline__ uint32_t codes(uint32_t w, __half2 za, __half2 zb) {
-  const uint32_t n = (I < 2 ? w : w >> 8) & ((I & 1) ? 0x00F000F0u : 0x000F000Fu);
-  const uint32_t x = n | ((I & 1) ? 0x54005400u : 0x64006400u);
-  const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&x), (I & 1) ? zb : za);
+  const uint32_t n = I < 2 ? w : w >> 8;
+  const __half2 d = (I & 1) ? __hsub2(high_nibbles(n), zb) : __hsub2(low_nibbles(n), za);
   return *reinterpret_cast<const uint32_t *>(&d);
 }
-// 1024 + z and 64 + z from the zeros in the low four bits of both halves (the rest clear).
+// 1024 + z and 64 + z from the zeros in the low four bits of both halves.
 __device__ __forceinline__ void zeros(uint32_t zz, __half2 *za, __half2 *zb) {
-  const uint32_t a = zz | 0x64006400u, b = zz << 4 | 0x54005400u;
-  *za = *reinterpret_cast<const __half2 *>(&a);
-  *zb = *reinterpret_cast<const __half2 *>(&b);
+  *za = low_nibbles(zz);
+  *zb = high_nibbles(zz * 16u);
 }
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-template <int D>
+template <int D, int NT>
 struct Ring {
-  static constexpr int kStages = D == 128 ? 3 : 6;
-  static constexpr int kBytes = kSplitWarps * kStages * Block<D>::kBytes;
+  static constexpr int kBytes = Shape<D, NT>::kWarps * Shape<D, NT>::kStages * Block<D>::kBytes;
   static constexpr int oSeq = (kBytes + 15) / 16 * 16;
   static constexpr int oBar = oSeq + (int)(sizeof(SeqTable) + 15) / 16 * 16;
-  static constexpr int kSmem = oBar + kSplitWarps * kStages * 8 + kSplitWarps * 8;
+  static constexpr int oScan = oBar + Shape<D, NT>::kWarps * Shape<D, NT>::kStages * 8;
+  static constexpr int kSmem = oScan + Shape<D, NT>::kWarps * 8;
+  static_assert(Shape<D, NT>::kWarps * Part<D, NT>::kFloats * 4 <= kBytes, "a part per warp in place of the ring");
   static_assert(kSmem <= 232448, "shared memory of the split kernel");
 };
 
 template <int D, int NT, bool BF16>
-__global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const AttnArgs a, float *parts) {
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
+    attn_split_kernel(const AttnArgs a, Join *joins, float *parts) {
   using B = Block<D>;
-  using R = Ring<D>;
-  constexpr int G = B::kGroups, S = R::kStages;
+  using R = Ring<D, NT>;
+  constexpr int G = B::kGroups, S = Shape<D, NT>::kStages;
+  constexpr int kSplitWarps = Shape<D, NT>::kWarps, kSplitThreads = Shape<D, NT>::kThreads;
   extern __shared__ __align__(128) unsigned char smem[];
   SeqTable &T = *reinterpret_cast<SeqTable *>(smem + R::oSeq);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -197,20 +276,24 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
     mbar_fence_init();
   }
   grid_dep_wait();
-  load_seqs(a, 8 * NT, T, reinterpret_cast<int64_t *>(smem + R::oBar + kSplitWarps * S * 8), blockIdx.x == 0);
+  load_seqs<kSplitWarps>(a, 8 * NT, T, reinterpret_cast<int64_t *>(smem + R::oScan));
   grid_dep_launch_next();
   const int heads = a.c.heads, g = a.q_heads / heads;
-  const int W = gridDim.x * kSplitWarps, w = blockIdx.x * kSplitWarps + warp;
-  const int64_t U = T.pre[a.count];
-  const int64_t u0 = first_unit(w, W, U), u1 = first_unit(w + 1, W, U);
-  if (u0 >= u1) return;
+  const int w = blockIdx.x * kSplitWarps + warp;
+  const Runs runs(T.pre[a.count], gridDim.x * kSplitWarps);
+  const int64_t u0 = runs.first(w), u1 = runs.first(w + 1);
+  const int64_t c0 = runs.first(blockIdx.x * kSplitWarps), c1 = runs.first((blockIdx.x + 1) * kSplitWarps);
+  if (u0 >= u1 && lane == 0) joins[w].w1 = -1;
+  if (c0 >= c1) return;  // the whole block
   const int nr = lane >> 2, j = lane & 3;  // row of a fragment, and quarter of its columns
 
+  const int units = (int)(u1 - u0);
+
   // ---- the blocks of 32 units, one per lane
-  int64_t base = u0;
+  int base = 0;
   const uint8_t *src;
   auto look_up = [&]() {
-    const int64_t u = base + lane;
+    const int64_t u = u0 + base + lane;
     src = nullptr;
     if (u < u1) {
       const int b = find_seq(T, a.count, u);
@@ -228,16 +311,16 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
     }
   };
   look_up();
-  int64_t next = u0;        // the unit to be fetched next
+  int next = 0;                   // the unit to be fetched next
   uint32_t holds = 0, phase = 0;  // per stage: it holds (or awaits) a block; the barrier's parity
-  int fill = 0;             // the stage it goes to
+  int fill = 0;                   // the stage it goes to
   auto fetch = [&]() {
-    if (next < u1) {
+    if (next < units) {
       if (next - base == 32) {
         base = next;
         look_up();
       }
-      const int from = (int)(next - base);
+      const int from = next - base;
       const uint64_t p = __shfl_sync(0xffffffffu, (unsigned long long)reinterpret_cast<uintptr_t>(src), from);
       if (p) {
         if (lane == 0) {
@@ -253,22 +336,41 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
   for (int i = 0; i < S; ++i) fetch();
 
   // ---- the segment (sequence, row tile, head) at hand
-  int b = find_seq(T, a.count, u0), L = 0, p0 = 0, np = 0, pg = 0, tile = 0, h = 0;
+  int b = u0 < u1 ? find_seq(T, a.count, u0) : 0, L = 0, p0 = 0, np = 0, pg = 0, tile = 0, h = 0;
   uint32_t qf[NT][G][8];
   float F[NT][2];  // score factors of columns 2 j, 2 j + 1
   int begin[NT][2], end[NT][2], some_begin = 0, all_end = 0;
   float O[NT][G][4][4], mx[NT][2], l[NT][2];
   int E = 0;
   int64_t seg_begin = 0;
-  {
+  auto clear = [&]() {
+    E = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      mx[t][0] = mx[t][1] = -kInf;
+      l[t][0] = l[t][1] = 0.0f;
+#pragma unroll
+      for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) O[t][gr][i][k] = 0.0f;
+    }
+  };
+  if (u0 < u1) {
     seq_pages(a, T.L[b], T.n[b], &p0, &np);
     const int64_t local = u0 - T.pre[b], seg = local / max(np, 1);
     pg = (int)(local - seg * max(np, 1));
     h = (int)(seg % heads);
     tile = (int)(seg / heads);
   }
-  const int rho = nr ^ ((nr >> 1) & 1);  // token of row nr: neighbours in banks apart
-  const uint32_t zsel = (j & 1) ? 0x1032u : 0x3210u;
+  // Tokens of a page in fragments: step s (of four) has tokens 8 nr + 2 s + odd in
+  // row nr and 8 nr + 2 s + 1 - odd in row nr + 8, so that a lane's eight params
+  // lie side by side.  Rows 2, 3, 6, 7 take the odd one first: the four
+  // tokens that a load of V codes touches then lie in different banks, two by two.
+  const int odd = (nr >> 1) & 1, vodd = j & 1;
+  const uint32_t psel = odd ? 0x1032u : 0x3210u;  // params of (row nr, row nr + 8)
+  const uint32_t zsel0 = vodd ? 0x7632u : 0x5410u, zsel1 = vodd ? 0x5410u : 0x7632u;
 
   auto begin_segment = [&](int64_t u) {
     seg_begin = u - pg;
@@ -279,7 +381,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
     const int pos_lo = L - n + row_lo / g, pos_hi = L - n + row_hi / g;
     all_end = a.causal ? pos_lo + 1 : L;                             // every row sees the tokens before
     some_begin = a.window > 0 ? max(0, pos_hi - a.window + 1) : 0;  // ... from here on
-    E = 0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int row = row_lo + 8 * t + nr;
@@ -308,7 +409,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
       // 2^e brings the largest into [2^10, 2^11); rows without a finite one stay
       int e = 0;
       if (BF16 && top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
-      const float up = BF16 ? __uint_as_float((uint32_t)(127 + e) << 23) : 1.0f;
+      // a negative scale turns the queries' sign, none makes them zeros: F > 0
+      float up = BF16 ? __uint_as_float((uint32_t)(127 + e) << 23) : 1.0f;
+      up = a.scale < 0.0f ? -up : a.scale == 0.0f ? 0.0f : up;
 #pragma unroll
       for (int gr = 0; gr < G; ++gr)
 #pragma unroll
@@ -316,7 +419,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
           qf[t][gr][2 * i] = pack_f16(x[gr][i] * up, x[gr][4 + i] * up);
           qf[t][gr][2 * i + 1] = pack_f16(x[gr][8 + i] * up, x[gr][12 + i] * up);
         }
-      const float Fr = a.scale * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23);
+      const float Fr =
+          a.scale == 0.0f ? 1.0f : fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-37f);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         F[t][c] = __shfl_sync(0xffffffffu, Fr, 4 * (2 * j + c));
@@ -324,90 +428,128 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
         const int pos = L - n + rc / g;
         end[t][c] = rc < rows ? (a.causal ? pos + 1 : L) : 0;
         begin[t][c] = a.window > 0 ? pos - a.window + 1 : 0;
-        mx[t][c] = -CUDART_INF_F;
-        l[t][c] = 0.0f;
       }
+    }
+    clear();
+  };
+
+  // 32 of a page's tokens, tok0 + 8 nr + 4 half .. (+ 3): two steps of the fragments
+  auto half_page = [&](const unsigned char *blk, int tok0, int half, bool plain) {
+    // params of the lane's tokens, (row nr, row nr + 8) of each step in a word
+    auto params = [&](int at, uint32_t *p) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(blk + at + nr * 16 + half * 8);
+      p[0] = __byte_perm(v.x, 0, psel);
+      p[1] = __byte_perm(v.y, 0, psel);
+    };
+    auto token = [&](int s, int hi) { return tok0 + 8 * nr + 4 * half + 2 * s + (hi ? 1 - odd : odd); };
+    auto sees = [&](int s, int t, int k) {
+      const int tok = token(s, k >> 1);
+      return tok >= begin[t][k & 1] && tok < end[t][k & 1];
+    };
+    uint32_t vs[G][2];
+#pragma unroll
+    for (int gr = 0; gr < G; ++gr) params(B::oPV + gr * kPage * 2, vs[gr]);
+    if (!plain) {  // what lies past the sequence's end may be anything
 #pragma unroll
       for (int gr = 0; gr < G; ++gr)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) O[t][gr][i][k] = 0.0f;
+        for (int s = 0; s < 2; ++s) {
+          if (token(s, 0) >= L) vs[gr][s] &= 0xFFFF0000u;
+          if (token(s, 1) >= L) vs[gr][s] &= 0x0000FFFFu;
+        }
     }
-  };
-
-  auto one_page = [&](const unsigned char *blk, int tok0) {
-    const bool plain = tok0 >= some_begin && tok0 + kPage <= all_end;
-    // the largest exponent of a value scale in the page's tokens
-    {
-      uint32_t top = 0;
+    // the largest exponent of a value scale
+    uint32_t top = 0;
+#pragma unroll
+    for (int gr = 0; gr < G; ++gr) top = __vmaxu2(top, __vmaxu2(vs[gr][0] & 0x7C007C00u, vs[gr][1] & 0x7C007C00u));
+    top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16)) >> 10;
+    if (top == 31) {
+      // A group stands for NaN: in rows that see its token its dimensions are
+      // lost (here and now: an unseen token's 0 times NaN must not count), the
+      // others' scales stay.
+      top = 0;
 #pragma unroll
       for (int gr = 0; gr < G; ++gr) {
-        const uint32_t v = *reinterpret_cast<const uint32_t *>(blk + B::oPV + gr * kPage * 2 + lane * 4);
-        uint32_t lo = v & 0xFFF0u, hi = (v >> 16) & 0xFFF0u;
-        if (tok0 + 2 * lane >= L || lo >= 0x7C00u) lo = 0;
-        if (tok0 + 2 * lane + 1 >= L || hi >= 0x7C00u) hi = 0;
-        top = max(top, max(lo, hi));
+        bool lost[NT][2] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            const uint32_t e = vs[gr][s] >> (16 * hi) & 0x7C00u;
+            if (e != 0x7C00u) {
+              top = max(top, e);
+              continue;
+            }
+            vs[gr][s] &= hi ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) lost[t][c] = lost[t][c] || sees(s, t, 2 * hi + c);
+          }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            if (__ballot_sync(0xffffffffu, lost[t][c]) & (0x11111111u << j))
+#pragma unroll
+              for (int i = 0; i < 4; ++i) O[t][gr][i][c] = O[t][gr][i][2 + c] = kInf - kInf;
       }
       top = __reduce_max_sync(0xffffffffu, top) >> 10;
-      if ((int)top > E) {
-        const float f = __uint_as_float((uint32_t)(127 + E - (int)top) << 23);
-        E = (int)top;
+    }
+    if ((int)top > E) {
+      const float f = __uint_as_float((uint32_t)(127 + E - (int)top) << 23);
+      E = (int)top;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          l[t][0] *= f;
-          l[t][1] *= f;
+      for (int t = 0; t < NT; ++t) {
+        l[t][0] *= f;
+        l[t][1] *= f;
 #pragma unroll
-          for (int gr = 0; gr < G; ++gr)
+        for (int gr = 0; gr < G; ++gr)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+          for (int k = 0; k < 4; ++k)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) O[t][gr][i][k] *= f;
-        }
+            for (int i = 0; i < 4; ++i) O[t][gr][i][k] *= f;
       }
     }
-    // scores (times log2 e) of tokens 16 s + rho, 16 s + 8 + rho for columns 2 j, 2 j + 1
-    float x[NT][4][4];
+    // scores (before the factor F) of the step's two tokens for columns 2 j, 2 j + 1
+    float x[NT][2][4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int t0 = 16 * s + rho;
+    for (int gr = 0; gr < G; ++gr) {
+      uint32_t ks[2];
+      params(B::oPK + gr * kPage * 2, ks);
 #pragma unroll
-      for (int gr = 0; gr < G; ++gr) {
-        const unsigned char *kp = blk + B::oK + t0 * B::kRow + gr * (kGrp / 2) + j * 8;
-        const uint2 r0 = *reinterpret_cast<const uint2 *>(kp), r1 = *reinterpret_cast<const uint2 *>(kp + 8 * B::kRow);
-        const uint32_t k0 = *reinterpret_cast<const uint16_t *>(blk + B::oPK + (gr * kPage + t0) * 2);
-        const uint32_t k1 = *reinterpret_cast<const uint16_t *>(blk + B::oPK + (gr * kPage + t0 + 8) * 2);
-        const float s0 = param_scale(k0), s1 = param_scale(k1);
+      for (int s = 0; s < 2; ++s) {
+        const unsigned char *kp = blk + B::oK + (8 * nr + 4 * half + 2 * s) * B::kRow + gr * (kGrp / 2) + j * 8;
+        const uint2 r0 = *reinterpret_cast<const uint2 *>(kp + odd * B::kRow);
+        const uint2 r1 = *reinterpret_cast<const uint2 *>(kp + (1 - odd) * B::kRow);
         __half2 a0, b0, a1, b1;
-        zeros((k0 & 15u) * 0x10001u, &a0, &b0);
-        zeros((k1 & 15u) * 0x10001u, &a1, &b1);
+        zeros(__byte_perm(ks[s], 0, 0x1010), &a0, &b0);
+        zeros(__byte_perm(ks[s], 0, 0x3232), &a1, &b1);
         float acc[NT][4];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
-#define TQ_STEP(I)                                                                                             \
-  {                                                                                                            \
-    const uint32_t A[4] = {codes<I>(r0.x, a0, b0), codes<I>(r1.x, a1, b1), codes<I>(r0.y, a0, b0),             \
-                           codes<I>(r1.y, a1, b1)};                                                            \
-    _Pragma("unroll") for (int t = 0; t < NT; ++t) mma_f16(acc[t], A, qf[t][gr][2 * I], qf[t][gr][2 * I + 1]); \
+#define TQ_STEP(I, MMA)                                                                                    \
+  {                                                                                                        \
+    const uint32_t A[4] = {codes<I>(r0.x, a0, b0), codes<I>(r1.x, a1, b1), codes<I>(r0.y, a0, b0),         \
+                           codes<I>(r1.y, a1, b1)};                                                        \
+    _Pragma("unroll") for (int t = 0; t < NT; ++t) MMA(acc[t], A, qf[t][gr][2 * I], qf[t][gr][2 * I + 1]); \
   }
-        TQ_STEP(0) TQ_STEP(1) TQ_STEP(2) TQ_STEP(3)
+        TQ_STEP(0, mma_f16_first) TQ_STEP(1, mma_f16) TQ_STEP(2, mma_f16) TQ_STEP(3, mma_f16)
 #undef TQ_STEP
+        const float2 sc = __half22float2(as_half2(ks[s] & 0xFFF0FFF0u));
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            x[t][s][k] = gr == 0 ? acc[t][k] * (k < 2 ? s0 : s1) : fmaf(acc[t][k], k < 2 ? s0 : s1, x[t][s][k]);
+            x[t][s][k] = gr == 0 ? acc[t][k] * (k < 2 ? sc.x : sc.y) : fmaf(acc[t][k], k < 2 ? sc.x : sc.y, x[t][s][k]);
       }
+    }
+    if (!plain) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[t][s][k] *= F[t][k & 1];
-          if (!plain) {
-            const int tok = tok0 + t0 + (k < 2 ? 0 : 8);
-            if (tok < begin[t][k & 1] || tok >= end[t][k & 1]) x[t][s][k] = -CUDART_INF_F;
-          }
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (!sees(s, t, k)) x[t][s][k] = -kInf;
     }
     // running maximum; probabilities
     bool grew = false;
@@ -416,16 +558,15 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float m = mx[t][c];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) m = fmaxf(m, fmaxf(x[t][s][c], x[t][s][2 + c]));
+        float m = fmaxf(fmaxf(x[t][0][c], x[t][0][2 + c]), fmaxf(x[t][1][c], x[t][1][2 + c]));
+        m = fmaxf(m, mx[t][c]);
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        const float at = m == -CUDART_INF_F ? 0.0f : m;
-        fac[t][c] = exp2_fast(mx[t][c] - at);
+        const float at = m == -kInf ? 0.0f : m * F[t][c];
+        fac[t][c] = exp2_fast(fmaf(mx[t][c], F[t][c], -at));
         grew = grew || m > mx[t][c];
         mx[t][c] = m;
-        ref[t][c] = at - (float)(29 - E);
+        ref[t][c] = (float)(29 - E) - at;
       }
     if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
@@ -443,49 +584,38 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          x[t][s][k] = exp2_fast(x[t][s][k] - ref[t][k & 1]);
+          x[t][s][k] = exp2_fast(fmaf(x[t][s][k], F[t][k & 1], ref[t][k & 1]));
           l[t][k & 1] += x[t][s][k];
         }
     // values
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int t0 = 16 * s + rho;
+    for (int gr = 0; gr < G; ++gr) {
+      // params of the columns' tokens 16 j + 4 half .., and of those 8 further on
+      const unsigned char *zp = blk + B::oPV + gr * kPage * 2 + j * 32 + half * 8;
+      const uint2 za = *reinterpret_cast<const uint2 *>(zp), zb = *reinterpret_cast<const uint2 *>(zp + 16);
 #pragma unroll
-      for (int gr = 0; gr < G; ++gr) {
-        float s0 = param_scale(*reinterpret_cast<const uint16_t *>(blk + B::oPV + (gr * kPage + t0) * 2));
-        float s1 = param_scale(*reinterpret_cast<const uint16_t *>(blk + B::oPV + (gr * kPage + t0 + 8) * 2));
+      for (int s = 0; s < 2; ++s) {
+        const float2 sc = __half22float2(as_half2(vs[gr][s] & 0xFFF0FFF0u));
         uint32_t bf[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          float p[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            p[k] = x[t][s][k] * (k < 2 ? s0 : s1);
-            // what a row does not see adds nothing, whatever it stands for
-            if (!plain) {
-              const int tok = tok0 + t0 + (k < 2 ? 0 : 8);
-              if (tok < begin[t][k & 1] || tok >= end[t][k & 1]) p[k] = 0.0f;
-            }
-          }
-          bf[t][0] = transpose8x8(pack_f16(p[0], p[1]));
-          bf[t][1] = transpose8x8(pack_f16(p[2], p[3]));
+          bf[t][0] = transpose8x8(pack_f16(x[t][s][0] * sc.x, x[t][s][1] * sc.x));
+          bf[t][1] = transpose8x8(pack_f16(x[t][s][2] * sc.y, x[t][s][3] * sc.y));
         }
-        // tokens of the column pairs: rho(2 j), rho(2 j + 1), and those + 8
-        const int ta = 2 * j + (j & 1), tb = 2 * j + 1 - (j & 1);
-        const unsigned char *vp = blk + B::oV + 16 * s * B::kRow + gr * (kGrp / 2) + nr * 4;
-        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(vp + ta * B::kRow);
-        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(vp + tb * B::kRow);
-        const uint32_t w2 = *reinterpret_cast<const uint32_t *>(vp + (ta + 8) * B::kRow);
-        const uint32_t w3 = *reinterpret_cast<const uint32_t *>(vp + (tb + 8) * B::kRow);
+        // the column pairs' tokens: those of rows 2 j, 2 j + 1, and of the rows 8 further on
+        const unsigned char *vp = blk + B::oV + (16 * j + 4 * half + 2 * s) * B::kRow + gr * (kGrp / 2) + nr * 4;
+        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(vp + vodd * B::kRow);
+        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(vp + (8 + vodd) * B::kRow);
+        const uint32_t w2 = *reinterpret_cast<const uint32_t *>(vp + (1 - vodd) * B::kRow);
+        const uint32_t w3 = *reinterpret_cast<const uint32_t *>(vp + (9 - vodd) * B::kRow);
         const uint32_t lo01 = __byte_perm(w0, w1, 0x5410), hi01 = __byte_perm(w0, w1, 0x7632);
         const uint32_t lo23 = __byte_perm(w2, w3, 0x5410), hi23 = __byte_perm(w2, w3, 0x7632);
-        const unsigned char *zp = blk + B::oPV + (gr * kPage + 16 * s + 2 * j) * 2;
         __half2 a0, b0, a1, b1;
-        zeros(__byte_perm(*reinterpret_cast<const uint32_t *>(zp) & 0x000F000Fu, 0, zsel), &a0, &b0);
-        zeros(__byte_perm(*reinterpret_cast<const uint32_t *>(zp + 16) & 0x000F000Fu, 0, zsel), &a1, &b1);
+        zeros(__byte_perm(s ? za.y : za.x, s ? zb.y : zb.x, zsel0), &a0, &b0);
+        zeros(__byte_perm(s ? za.y : za.x, s ? zb.y : zb.x, zsel1), &a1, &b1);
 #define TQ_STEP(I)                                                                                 \
   {                                                                                                \
     const uint32_t A[4] = {codes<I>(lo01, a0, b0), codes<I>(hi01, a0, b0), codes<I>(lo23, a1, b1), \
@@ -499,20 +629,51 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
   };
 
   // the segment's results, or the warp's part of them
-  auto end_segment = [&](int64_t u) {
-    const bool whole = seg_begin >= u0 && seg_begin + max(np, 1) <= u1;
-    float *part = parts + ((int64_t)w * 2 + (seg_begin <= u0 ? 0 : 1)) * Part<D, NT>::kFloats;
-    (void)u;
+  // does the block's run (of several warps) lie inside one segment? its parts then become one
+  bool one_segment = false;
+  if (c1 > runs.first(blockIdx.x * kSplitWarps + 1)) {
+    const int bb = find_seq(T, a.count, c0);
+    int q0, n;
+    seq_pages(a, T.L[bb], T.n[bb], &q0, &n);
+    n = max(n, 1);
+    const int64_t s0 = T.pre[bb] + (c0 - T.pre[bb]) / n * n;
+    one_segment = s0 + n >= c1;
+  }
+  auto end_segment = [&]() {
+    const int64_t seg_end = seg_begin + max(np, 1);
+    const bool whole = seg_begin >= u0 && seg_end <= u1 && !one_segment;
+    float *part = one_segment ? reinterpret_cast<float *>(smem) + warp * Part<D, NT>::kFloats
+                              : parts + ((int64_t)w * 2 + (seg_begin <= u0 ? 0 : 1)) * Part<D, NT>::kFloats;
+    if (seg_begin <= u0 && units > 0 && lane == 0) {
+      Join J;
+      J.w0 = w - 1;
+      J.w1 = -1;
+      const int64_t f0 = w > 0 ? runs.first(w - 1) : 0;
+      if (seg_begin < u0 && f0 <= seg_begin) {  // the worker before begins the segment
+        J.w1 = runs.worker(seg_end - 1);
+        J.slot0 = seg_begin <= f0 ? 0 : 1;
+        J.f0 = (w - 1) / kSplitWarps;
+        if (runs.first(J.f0 * kSplitWarps) < seg_begin) ++J.f0;
+        J.f1 = J.w1 / kSplitWarps;
+        if (runs.first((J.f1 + 1) * kSplitWarps) <= seg_end) ++J.f1;
+        J.row0 = tile * Part<D, NT>::kRows;
+        J.rows = T.n[b] * g;
+        J.q0 = T.q0[b];
+        J.h = h;
+      }
+      joins[w] = J;
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
+        const int rows = one_segment ? 0x7fffffff : T.n[b] * g;
         float sum = l[t][c];
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int r = 8 * t + 2 * j + c, row = tile * Part<D, NT>::kRows + r;
-        const bool there = row < T.n[b] * g;
-        const float m = mx[t][c] == -CUDART_INF_F ? -CUDART_INF_F : mx[t][c] - (float)(29 - E);
+        const bool there = row < rows;
+        const float m = mx[t][c] == -kInf ? -kInf : mx[t][c] * F[t][c] - (float)(29 - E);
         const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
         const int64_t token = T.q0[b] + (there ? row / g : 0);
         const int head = h * g + row % g;
@@ -524,11 +685,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
             o[i] = O[t][gr][i][c] * inv;
             o[4 + i] = O[t][gr][i][2 + c] * inv;
           }
-          if (!whole) {
+          if (!whole && there) {
             float4 *dst = reinterpret_cast<float4 *>(part + r * D + gr * kGrp + 8 * nr);
             dst[0] = make_float4(o[0], o[1], o[2], o[3]);
             dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-          } else if (there) {
+          } else if (whole && there) {
             uint32_t v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = pack_out<BF16>(o[2 * i], o[2 * i + 1]);
@@ -536,12 +697,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
                 make_uint4(v[0], v[1], v[2], v[3]);
           }
         }
-        if (nr == 0) {
+        if (nr == 0 && there) {
           if (!whole) {
             part[Part<D, NT>::kRows * D + r] = m;
             part[Part<D, NT>::kRows * (D + 1) + r] = sum;
-          } else if (there && a.lse) {
-            a.lse[token * a.q_heads + head] = sum == 0.0f ? -CUDART_INF_F : kLn2 * (m + log2f(sum));
+          } else if (a.lse) {
+            a.lse[token * a.q_heads + head] = sum == 0.0f ? -kInf : kLn2 * (m + log2f(sum));
           }
         }
       }
@@ -549,22 +710,26 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
 
   bool fresh = true;
   int stage = 0;
-  for (int64_t u = u0; u < u1; ++u) {
-    if (fresh) begin_segment(u);
+  for (int i = 0; i < units; ++i) {
+    if (fresh) begin_segment(u0 + i);
     fresh = false;
     if (holds >> stage & 1) {
       holds &= ~(1u << stage);
       if (!__all_sync(0xffffffffu, mbar_wait(&bars[stage], phase >> stage & 1))) break;
       phase ^= 1u << stage;
-      one_page(ring + stage * B::kBytes, (p0 + pg) * kPage);
+      const int tok0 = (p0 + pg) * kPage;
+      const bool plain = tok0 >= some_begin && tok0 + kPage <= all_end;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) half_page(ring + stage * B::kBytes, tok0, half, plain);
       __syncwarp();
     }
     fetch();  // into the stage just read
     stage = stage + 1 == S ? 0 : stage + 1;
-    if (++pg >= np || u + 1 == u1) {
-      end_segment(u);
+    if (++pg >= np || i + 1 == units) {
+      if (!one_segment) end_segment();
       fresh = true;
-      if (pg >= np && u + 1 < u1) {
+      if (pg >= np && i + 1 < units) {
+        const int64_t u = u0 + i;
         pg = 0;
         if (++h == heads) {
           h = 0;
@@ -581,94 +746,61 @@ __global__ void __launch_bounds__(kSplitThreads, 1) attn_split_kernel(const Attn
   // after a wait that ran out: no copy may land in a block that is gone
   for (int i = 0; i < S; ++i)
     if (holds >> i & 1) mbar_wait(&bars[i], phase >> i & 1);
-}
 
-// Joins the parts of the segments that several workers shared: block (segment,
-// row) pairs in turn, eight groups of lanes over the parts, then over the block.
-template <int D, int NT, bool BF16>
-__global__ void __launch_bounds__(kSplitThreads) attn_combine_kernel(const AttnArgs a, const float *parts, int W) {
-  constexpr int RT = Part<D, NT>::kRows, LPD = D / 4, GROUPS = kSplitThreads / LPD;
-  __shared__ SeqTable T;
-  __shared__ int64_t part[kSplitWarps];
-  __shared__ float4 so[GROUPS][LPD];
-  __shared__ float sm[GROUPS], sl[GROUPS];
-  const int tid = threadIdx.x, grp = tid / LPD, lane = tid % LPD;
-  const int g = a.q_heads / a.c.heads;
-  load_seqs(a, RT, T, part, false);
-  grid_dep_wait();  // the lists are inputs of the split kernel too: only its parts are new
-  const int64_t U = T.pre[a.count];
-  // A segment that several workers share holds a worker's first unit inside it:
-  // the first worker with units after the one that begins it stands for it.
-  // Items are (worker, row); every warp looks at 32 of the block's at once.
-  struct Shared {
-    int64_t seg, s0;
-    int b, w0, w1;
-  };
-  auto shared_by = [&](int wi, Shared *s) {
-    const int64_t ub = first_unit(wi, W, U);
-    if (ub >= U || first_unit(wi + 1, W, U) == ub) return false;
-    s->b = find_seq(T, a.count, ub);
-    int p0, np;
-    seq_pages(a, T.L[s->b], T.n[s->b], &p0, &np);
-    np = max(np, 1);
-    s->seg = (ub - T.pre[s->b]) / np;
-    s->s0 = T.pre[s->b] + s->seg * np;
-    if (s->s0 >= ub) return false;  // begins here
-    s->w0 = worker_of(s->s0, W, U);
-    s->w1 = worker_of(s->s0 + np - 1, W, U);
-    int first = s->w0 + 1;
-    while (first < wi && first_unit(first + 1, W, U) == first_unit(first, W, U)) ++first;
-    return first == wi;
-  };
-  const int64_t items = (int64_t)W * RT;
-  for (int64_t from = blockIdx.x; from < items; from += (int64_t)gridDim.x * 32) {
-    const int64_t mine = from + (int64_t)(tid & 31) * gridDim.x;
-    Shared s;
-    uint32_t todo = __ballot_sync(0xffffffffu, mine < items && mine >= RT && shared_by((int)(mine / RT), &s));
-    for (; todo; todo &= todo - 1) {
-      const int64_t it = from + (int64_t)(__ffs(todo) - 1) * gridDim.x;
-      const int r = (int)(it % RT);
-      shared_by((int)(it / RT), &s);
-      const int h = (int)(s.seg % a.c.heads), row = (int)(s.seg / a.c.heads) * RT + r;
-      if (row >= T.n[s.b] * g) continue;
-      float m = -CUDART_INF_F, l = 0.0f;
-      float4 o = make_float4(0, 0, 0, 0);
-      auto join = [&](float pm, float pl, const float4 &po) {
-        const float nm = fmaxf(m, pm), at = nm == -CUDART_INF_F ? 0.0f : nm;
-        const float fa = exp2_fast(m - at), fb = exp2_fast(pm - at);
-        l = l * fa + pl * fb;
-        o.x = o.x * fa + po.x * fb;
-        o.y = o.y * fa + po.y * fb;
-        o.z = o.z * fa + po.z * fb;
-        o.w = o.w * fa + po.w * fb;
-        m = nm;
-      };
-      for (int w = s.w0 + grp; w <= s.w1; w += GROUPS) {
-        const int64_t f = first_unit(w, W, U);
-        if (first_unit(w + 1, W, U) == f) continue;
-        const float *p = parts + ((int64_t)w * 2 + (s.s0 <= f ? 0 : 1)) * Part<D, NT>::kFloats;
-        join(p[RT * D + r], p[RT * (D + 1) + r], reinterpret_cast<const float4 *>(p + r * D)[lane]);
-      }
-      so[grp][lane] = o;
-      if (lane == 0) {
-        sm[grp] = m;
-        sl[grp] = l;
-      }
-      __syncthreads();
-      if (grp == 0) {
+  if (!one_segment) return;  // the same for the whole block
+  __syncthreads();           // the ring is free
+  if (units == 0) clear();
+  end_segment();
+  __syncthreads();
+  float *own = parts + (int64_t)blockIdx.x * kSplitWarps * 2 * Part<D, NT>::kFloats;
+  for (int k = tid; k < Part<D, NT>::kRows * Part<D, NT>::kLanes; k += kSplitThreads) {
+    const int r = k / Part<D, NT>::kLanes, ln = k % Part<D, NT>::kLanes;
+    Soft f;
 #pragma unroll
-        for (int k = 1; k < GROUPS; ++k) join(sm[k], sl[k], so[k][lane]);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const int64_t token = T.q0[s.b] + row / g;
-        const int head = h * g + row % g;
-        *reinterpret_cast<uint2 *>(a.out + token * a.out_stride + head * D + 4 * lane) =
-            make_uint2(pack_out<BF16>(o.x * inv, o.y * inv), pack_out<BF16>(o.z * inv, o.w * inv));
-        if (lane == 0 && a.lse)
-          a.lse[token * a.q_heads + head] = l == 0.0f ? -CUDART_INF_F : kLn2 * (m + log2f(l));
-      }
-      __syncthreads();
+    for (int q = 0; q < kSplitWarps; ++q)
+      f.template join<D, NT>(reinterpret_cast<const float *>(smem) + q * Part<D, NT>::kFloats, r, ln);
+    reinterpret_cast<float4 *>(own + r * D)[ln] = f.o;
+    if (ln == 0) {
+      own[Part<D, NT>::kRows * D + r] = f.m;
+      own[Part<D, NT>::kRows * (D + 1) + r] = f.l;
     }
   }
+}
+
+// Joins the parts of the segments that several workers shared, each as joins[]
+// says; a thread has four dimensions of a row.
+template <int D, int NT, bool BF16>
+__global__ void __launch_bounds__(Part<D, NT>::kRows *Part<D, NT>::kLanes)
+    attn_combine_kernel(const AttnArgs a, const Join *joins, const float *parts) {
+  constexpr int RT = Part<D, NT>::kRows, kAhead = 8, kSplitWarps = Shape<D, NT>::kWarps;
+  const int r = threadIdx.x / Part<D, NT>::kLanes, lane = threadIdx.x % Part<D, NT>::kLanes;
+  grid_dep_wait();
+  const Join J = joins[blockIdx.x];
+  if (J.w1 < 0 || J.row0 + r >= J.rows) return;
+  // parts: workers up to the first block that lies inside, a part per such block, workers after them
+  const int blocks = max(J.f1 - J.f0, 0);
+  const int before = blocks ? J.f0 * kSplitWarps - J.w0 : J.w1 + 1 - J.w0;
+  const int n = blocks ? before + blocks + max(J.w1 + 1 - J.f1 * kSplitWarps, 0) : before;
+  Soft f;
+  for (int i = 0; i < n; i += kAhead) {
+    float m[kAhead], l[kAhead];
+    float4 o[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int v = min(i + k, n - 1);
+      const int w = v < before            ? J.w0 + v
+                    : v < before + blocks ? (J.f0 + v - before) * kSplitWarps
+                                          : J.f1 * kSplitWarps + v - before - blocks;
+      const float *p = parts + ((int64_t)w * 2 + (w == J.w0 ? J.slot0 : 0)) * Part<D, NT>::kFloats;
+      m[k] = p[RT * D + r];
+      l[k] = p[RT * (D + 1) + r];
+      o[k] = reinterpret_cast<const float4 *>(p + r * D)[lane];
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k < n) f.join(m[k], l[k], o[k]);
+  }
+  f.template write<D, BF16>(a, J.q0, J.row0 + r, J.h, lane);
 }
 
 // SMs of the current device (asked once per device).
@@ -689,32 +821,36 @@ int sm_count() {
 }
 
 inline size_t split_ws_bytes(int D, int NT) {
-  return (size_t)sm_count() * kSplitWarps * 2 * (8 * NT) * (D + 2) * 4;
+  const int warps = NT == 1 ? Shape<128, 1>::kWarps : Shape<128, 2>::kWarps;
+  return (size_t)sm_count() * warps * (sizeof(Join) + 2 * (8 * NT) * (D + 2) * 4);
 }
 inline int split_tiles(int max_q, int group) { return (int64_t)max_q * group <= 8 ? 1 : 2; }
 
 template <int D, int NT, bool BF16>
-cudaError_t launch_split(AttnArgs a, float *parts, cudaStream_t st) {
-  const int ctas = sm_count();
+cudaError_t launch_split(AttnArgs a, void *ws, cudaStream_t st) {
+  const int ctas = sm_count(), workers = ctas * Shape<D, NT>::kWarps;
+  Join *joins = static_cast<Join *>(ws);
+  float *parts = reinterpret_cast<float *>(joins + workers);
   const int count = a.count;
   const int32_t *slots = a.slots, *indptr = a.indptr;
   for (int b = 0; b < count; b += kMaxSeqs) {
     a.count = std::min(kMaxSeqs, count - b);
     a.slots = slots + b;
     a.indptr = indptr + b;
-    cudaError_t e = launch_big_smem(attn_split_kernel<D, NT, BF16>, ctas, kSplitThreads, Ring<D>::kSmem, st, a, parts);
+    cudaError_t e = launch_big_smem(attn_split_kernel<D, NT, BF16>, ctas, Shape<D, NT>::kThreads,
+                                    Ring<D, NT>::kSmem, st, a, joins, parts);
     if (e != cudaSuccess) return e;
-    e = launch_dependent(attn_combine_kernel<D, NT, BF16>, dim3(ctas * 2), kSplitThreads, st, a, (const float *)parts,
-                         ctas * kSplitWarps);
+    e = launch_dependent(attn_combine_kernel<D, NT, BF16>, dim3(workers), Part<D, NT>::kRows * Part<D, NT>::kLanes, st,
+                         a, (const Join *)joins, (const float *)parts);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
 template <int D>
-cudaError_t split_attention(const AttnArgs &a, int NT, bool bf16, float *parts, cudaStream_t st) {
-  if (NT == 1) return bf16 ? launch_split<D, 1, true>(a, parts, st) : launch_split<D, 1, false>(a, parts, st);
-  return bf16 ? launch_split<D, 2, true>(a, parts, st) : launch_split<D, 2, false>(a, parts, st);
+cudaError_t split_attention(const AttnArgs &a, int NT, bool bf16, void *ws, cudaStream_t st) {
+  if (NT == 1) return bf16 ? launch_split<D, 1, true>(a, ws, st) : launch_split<D, 1, false>(a, ws, st);
+  return bf16 ? launch_split<D, 2, true>(a, ws, st) : launch_split<D, 2, false>(a, ws, st);
 }
 
 TQ_STATUS_ACCESSOR(read_status_kv4_attention)
@@ -757,9 +893,8 @@ tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t count, 
                       q_stride, out_stride, scale,  d_status};
   cudaStream_t st = (cudaStream_t)stream;
   const int nt = split_tiles(max_q, q_heads / c->heads);
-  float *parts = static_cast<float *>(workspace);
-  return from_cuda(c->dim == 128 ? split_attention<128>(a, nt, dtype == TQ_BF16, parts, st)
-                                 : split_attention<64>(a, nt, dtype == TQ_BF16, parts, st));
+  return from_cuda(c->dim == 128 ? split_attention<128>(a, nt, dtype == TQ_BF16, workspace, st)
+                                 : split_attention<64>(a, nt, dtype == TQ_BF16, workspace, st));
 }
 
 }  // extern "C"
