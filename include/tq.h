@@ -655,7 +655,7 @@ TQ_API tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t 
  * the codes [16][64] (column 2 b of the group in the low half of byte b), then
  * (scale, minimum) [16]; rows past N are zeros. */
 typedef struct {
-  int32_t N, K;         /* K a multiple of 128 */
+  int32_t N, K;         /* K a multiple of 128, at most 96000 */
   const uint8_t *tiles; /* 16-byte aligned, tq_w4_bytes(N, K) bytes */
 } tq_w4_weight;
 TQ_API size_t tq_w4_bytes(int32_t N, int32_t K);

@@ -1,6 +1,8 @@
 // tq_w4.cu - 4-bit weights with group scales: packing, quantization and the
 // product with a few tokens' activations (formats and definitions in
 // include/tq.h).
+#include <atomic>
+
 #include "tq_kv4.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -15,7 +17,7 @@ constexpr int kRows = 16;                       // rows of a tile
 constexpr int kRowBytes = kGroup / 2;           // code bytes of a row in a tile
 constexpr int kCodes = kRows * kRowBytes;       // 1024
 constexpr int kTile = kCodes + kRows * 4;       // 1088
-constexpr int kMaxK = 1 << 20, kMaxN = 1 << 24;
+constexpr int kMaxK = 96000, kMaxN = 1 << 24;  // a token's x fits a block's shared memory
 
 inline int64_t tiles_bytes(int N, int K) { return (int64_t)((N + kRows - 1) / kRows) * (K / kGroup) * kTile; }
 inline bool good_shape(int N, int K) { return N >= 1 && N <= kMaxN && K >= kGroup && K % kGroup == 0 && K <= kMaxK; }
@@ -110,36 +112,285 @@ __global__ void __launch_bounds__(256)
       make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 
-// One warp per (token, row).
-template <bool F32>
-__global__ void __launch_bounds__(256)
-    linear_simple_kernel(int M, int N, int K, const uint8_t *__restrict__ tiles, const uint16_t *__restrict__ x,
-                         void *y) {
+// ------------------------------------------------------------------------
+// linear_kernel: y = x W^T for up to 8 NT tokens.
+//
+// Mathematics.  y_n = sum_g s_ng sum_k x_k (c - 8)_nk + (m_ng + 8 s_ng) sum_k x_k:
+// codes go to the tensor cores as the integers c - 8, exact, scales and minima
+// meet fp32 sums, so no weight is rounded.  A nibble OR-ed into the low bits of
+// fp16 1024 (64 from the next four bits) and a packed subtraction of 1032 (72)
+// give two codes in two instructions and a half.
+//
+// Bound by the weights' bytes; mma.sync with the rows of W as its rows and the
+// tokens as its eight columns takes the decoded codes from registers.
+// Split.  A block (one per SM, 16 warps) has a run of whole row tiles, its warps
+// equal runs of their (tile, group) units: a unit is 1088 bytes in a row, which a
+// warp reads straight into registers three units ahead (50 KB under way per
+// SM).  A tile that several warps share is summed in shared memory in the order
+// of the warps.  Every block holds x in operand order.
+constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kAhead = 3;
+
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
+// c - 8 of nibble I of both 16-bit halves.
+template <int I>
+__device__ __forceinline__ uint32_t codes(uint32_t w) {
+  const uint32_t n = I < 2 ? w : w >> 8;
+  const uint32_t x = (I & 1) ? and_or(n, 0x00F000F0u, 0x54005400u) : and_or(n, 0x000F000Fu, 0x64006400u);
+  const uint32_t o = (I & 1) ? 0x54805480u : 0x64086408u;  // 72, 1032
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&o));
+  return *reinterpret_cast<const uint32_t *>(&d);
+}
+__device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Shared memory: x in operand order ([group][4][token][4 lanes] 16 bytes), the
+// sums of x per group and token ([group][8 NT] floats), two parts per warp
+// ([16 rows][8 NT] floats each).
+template <int NT>
+struct Lay {
+  static constexpr int kPart = kRows * 8 * NT;  // floats
+  static constexpr int kParts = kWarps * 2 * kPart * 4;
+  static int64_t bytes(int tokens, int K) {
+    return (int64_t)tokens * K * 2 + (int64_t)(K / kGroup) * 8 * NT * 4 + kParts;
+  }
+};
+constexpr int kMaxSmem = 232448;
+
+struct Unit {
+  uint4 c0, c1;     // codes of rows nr, nr + 8, 32 columns from 32 j
+  uint32_t p0, p1;  // their scales and minima
+};
+__device__ __forceinline__ uint4 ld_stream(const void *p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
+template <int NT, bool F32>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_kernel(int M, int N, int K, const uint8_t *__restrict__ tiles, const uint16_t *__restrict__ x, void *y) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int G = K / kGroup, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nr = lane >> 2, j = lane & 3;
+  unsigned char *xs = smem;
+  float *xsum = reinterpret_cast<float *>(smem + (int64_t)M * K * 2);
+  float *parts = xsum + G * 8 * NT;
+  // the block's tiles, the warp's units of them
+  const int ntiles = (N + kRows - 1) / kRows;
+  const int t0 = (int)((int64_t)ntiles * blockIdx.x / gridDim.x), t1 = (int)((int64_t)ntiles * (blockIdx.x + 1) / gridDim.x);
+  const int units = (t1 - t0) * G;
+  const int each = units / kWarps, more = units % kWarps;
+  const int u0 = each * warp + min(warp, more), u1 = u0 + each + (warp < more);
+  const uint8_t *at = tiles + ((int64_t)t0 * G + u0) * kTile + lane * 16;
   grid_dep_wait();
-  const int G = K / kGroup, lane = threadIdx.x & 31;
-  const int64_t id = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  if (id >= (int64_t)M * N) return;
-  const int n = (int)(id % N), m = (int)(id / N);
-  float acc = 0.0f;
-  for (int g = 0; g < G; ++g) {
-    const uint8_t *t = tiles + ((int64_t)(n / kRows) * G + g) * kTile;
-    const uint32_t c = *reinterpret_cast<const uint16_t *>(t + (n % kRows) * kRowBytes + lane * 2);
-    const uint32_t p = *reinterpret_cast<const uint32_t *>(t + kCodes + (n % kRows) * 4);
-    const float s = __half2float(__ushort_as_half((unsigned short)p)),
-                mn = __half2float(__ushort_as_half((unsigned short)(p >> 16)));
+  Unit q[kAhead];
+  auto load = [&](Unit &v, int u) {
+    if (u < u1) {
+      const uint8_t *p = at + (int64_t)(u - u0) * kTile;
+      v.c0 = ld_stream(p);
+      v.c1 = ld_stream(p + kCodes / 2);
+      const uint32_t *s = reinterpret_cast<const uint32_t *>(p - lane * 16 + kCodes);
+      v.p0 = __ldg(s + nr);
+      v.p1 = __ldg(s + nr + 8);
+    }
+  };
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      acc += __half2float(__ushort_as_half(x[(int64_t)m * K + g * kGroup + lane * 4 + i])) *
-             fmaf(s, (float)((c >> (4 * i)) & 15u), mn);
+  for (int i = 0; i < kAhead; ++i) load(q[i], u0 + i);
+  // x: eight threads per (group, token), 16 columns each
+  for (int it = tid; it < G * M * 8; it += kThreads) {
+    const int part = it & 7, m = (it >> 3) % M, g = (it >> 3) / M, jj = part >> 1, p = part & 1;
+    const uint4 *src = reinterpret_cast<const uint4 *>(x + (int64_t)m * K + g * kGroup + 32 * jj + 16 * p);
+    const uint4 a = __ldg(src), b = __ldg(src + 1);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};  // columns 2 i, 2 i + 1
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+      sum += f.x + f.y;
+    }
+    // step i takes columns (i, 4 + i) and (8 + i, 12 + i)
+    uint4 *dst = reinterpret_cast<uint4 *>(xs + ((int64_t)(g * 4 + 2 * p) * M + m) * 64 + jj * 16);
+    dst[0] = make_uint4(__byte_perm(w[0], w[2], 0x5410), __byte_perm(w[4], w[6], 0x5410),
+                        __byte_perm(w[0], w[2], 0x7632), __byte_perm(w[4], w[6], 0x7632));
+    dst[(int64_t)M * 4] = make_uint4(__byte_perm(w[1], w[3], 0x5410), __byte_perm(w[5], w[7], 0x5410),
+                                     __byte_perm(w[1], w[3], 0x7632), __byte_perm(w[5], w[7], 0x7632));
+    const uint32_t lanes = 0xffu << (lane & 24);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(lanes, sum, d);
+    if (part == 0) xsum[g * 8 * NT + m] = sum;
   }
+  for (int it = tid; it < G * (8 * NT - M); it += kThreads)  // tokens that are not there
+    xsum[it / (8 * NT - M) * 8 * NT + M + it % (8 * NT - M)] = 0.0f;
+  __syncthreads();
+
+  int tile = G > 0 ? u0 / G : 0, g = u0 - tile * G;
+  const int first_tile = tile;
+  float Y[NT][4];
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-  if (lane == 0) {
+  for (int t = 0; t < NT; ++t) Y[t][0] = Y[t][1] = Y[t][2] = Y[t][3] = 0.0f;
+  const unsigned char *xl = xs + nr * 64 + j * 16;
+  auto one = [&](Unit &v, int u) {
+    const uint32_t wa[4] = {v.c0.x, v.c0.y, v.c0.z, v.c0.w}, wb[4] = {v.c1.x, v.c1.y, v.c1.z, v.c1.w};
+    const uint32_t p0 = v.p0, p1 = v.p1;
+    load(v, u + kAhead);
+    float acc[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
+    const unsigned char *xg = xl + (int64_t)g * 4 * M * 64;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+#pragma unroll
+      for (int ip = 0; ip < 2; ++ip) {
+        uint4 b[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          b[t] = make_uint4(0, 0, 0, 0);
+          if (8 * t + nr < M) b[t] = *reinterpret_cast<const uint4 *>(xg + (2 * p + ip) * M * 64 + t * 512);
+        }
+        if (ip == 0) {
+          const uint32_t A0[4] = {codes<0>(wa[2 * p]), codes<0>(wb[2 * p]), codes<0>(wa[2 * p + 1]), codes<0>(wb[2 * p + 1])};
+          const uint32_t A1[4] = {codes<1>(wa[2 * p]), codes<1>(wb[2 * p]), codes<1>(wa[2 * p + 1]), codes<1>(wb[2 * p + 1])};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A0, b[t].x, b[t].y);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A1, b[t].z, b[t].w);
+        } else {
+          const uint32_t A0[4] = {codes<2>(wa[2 * p]), codes<2>(wb[2 * p]), codes<2>(wa[2 * p + 1]), codes<2>(wb[2 * p + 1])};
+          const uint32_t A1[4] = {codes<3>(wa[2 * p]), codes<3>(wb[2 * p]), codes<3>(wa[2 * p + 1]), codes<3>(wb[2 * p + 1])};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A0, b[t].x, b[t].y);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A1, b[t].z, b[t].w);
+        }
+      }
+    }
+    const float2 q0 = __half22float2(*reinterpret_cast<const __half2 *>(&p0));
+    const float2 q1 = __half22float2(*reinterpret_cast<const __half2 *>(&p1));
+    const float m0 = fmaf(8.0f, q0.x, q0.y), m1 = fmaf(8.0f, q1.x, q1.y);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float2 s = *reinterpret_cast<const float2 *>(xsum + (g * NT + t) * 8 + 2 * j);
+      Y[t][0] = fmaf(acc[t][0], q0.x, fmaf(m0, s.x, Y[t][0]));
+      Y[t][1] = fmaf(acc[t][1], q0.x, fmaf(m0, s.y, Y[t][1]));
+      Y[t][2] = fmaf(acc[t][2], q1.x, fmaf(m1, s.x, Y[t][2]));
+      Y[t][3] = fmaf(acc[t][3], q1.x, fmaf(m1, s.y, Y[t][3]));
+    }
+    // the end of a tile, or of the run
+    if (++g == G || u + 1 == u1) {
+      const bool whole = g == G && u + 1 - G >= u0;
+      const int n = (t0 + tile) * kRows;
+      float *part = parts + (2 * warp + (tile == first_tile ? 0 : 1)) * Lay<NT>::kPart;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = nr + (k < 2 ? 0 : 8), m = 8 * t + 2 * j + (k & 1);
+          if (!whole) {
+            part[r * 8 * NT + m] = Y[t][k];
+          } else if (n + r < N && m < M) {
+            if (F32)
+              static_cast<float *>(y)[(int64_t)m * N + n + r] = Y[t][k];
+            else
+              static_cast<uint16_t *>(y)[(int64_t)m * N + n + r] = __half_as_ushort(__float2half_rn(Y[t][k]));
+          }
+          Y[t][k] = 0.0f;
+        }
+      if (g == G) {
+        g = 0;
+        ++tile;
+      }
+    }
+  };
+  for (int u = u0; u < u1; u += kAhead) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (u + i < u1) one(q[i], u + i);
+  }
+  __syncthreads();
+  // tiles that several warps share
+  const int head = (each + 1) * more;
+  auto owner = [&](int u) { return u < head ? u / (each + 1) : more + (u - head) / each; };
+  for (int it = tid; it < (t1 - t0) * kRows * M; it += kThreads) {
+    const int r = it % kRows, m = it / kRows % M, t = it / (kRows * M);
+    const int w0 = owner(t * G), w1 = owner(t * G + G - 1), n = (t0 + t) * kRows + r;
+    if (w0 == w1 || n >= N) continue;
+    float sum = 0.0f;
+    for (int w = w0; w <= w1; ++w) {
+      const int f = (each * w + min(w, more)) / G;  // the tile that worker w begins in
+      sum += parts[(2 * w + (f == t ? 0 : 1)) * Lay<NT>::kPart + r * 8 * NT + m];
+    }
     if (F32)
-      static_cast<float *>(y)[id] = acc;
+      static_cast<float *>(y)[(int64_t)m * N + n] = sum;
     else
-      static_cast<uint16_t *>(y)[id] = __half_as_ushort(__float2half_rn(acc));
+      static_cast<uint16_t *>(y)[(int64_t)m * N + n] = __half_as_ushort(__float2half_rn(sum));
   }
+}
+
+// Tokens of a pass: as many n-tiles as the call has tokens for and x fits with.
+struct Pass {
+  int nt, tokens;
+};
+Pass pass_of(int M, int K) {
+  auto most = [&](int nt, int64_t fixed) {
+    const int64_t room = (kMaxSmem - fixed) / (2 * (int64_t)K);
+    return (int)(room < 8 * nt ? room : 8 * nt);
+  };
+  const int64_t G = K / kGroup;
+  const int m4 = most(4, Lay<4>::kParts + G * 128), m2 = most(2, Lay<2>::kParts + G * 64), m1 = most(1, Lay<1>::kParts + G * 32);
+  if (M > 16 && m4 > m2 && m4 > 16) return {4, m4};
+  if (M > 8 && m2 > m1) return {2, m2};
+  return {1, m1};
+}
+
+int sm_count() {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 152;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (!n) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+      (void)cudaGetLastError();
+      return 152;
+    }
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+template <int NT, bool F32>
+cudaError_t launch_linear(int M, int N, int K, const uint8_t *tiles, const uint16_t *x, void *y, cudaStream_t st) {
+  const cudaError_t e =
+      cudaFuncSetAttribute(linear_kernel<NT, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  if (e != cudaSuccess) return e;
+  const int ntiles = (N + kRows - 1) / kRows, sms = sm_count();
+  return launch_dependent_cluster(linear_kernel<NT, F32>, dim3(ntiles < sms ? ntiles : sms), 1, kThreads,
+                                  (int)Lay<NT>::bytes(M, K), st, M, N, K, tiles, x, y);
+}
+template <bool F32>
+cudaError_t linear_passes(int M, int N, int K, const uint8_t *tiles, const uint16_t *x, void *y, cudaStream_t st) {
+  const Pass p = pass_of(M, K);
+  for (int m = 0; m < M; m += p.tokens) {
+    const int n = M - m < p.tokens ? M - m : p.tokens;
+    const uint16_t *xm = x + (int64_t)m * K;
+    void *ym = F32 ? (void *)(static_cast<float *>(y) + (int64_t)m * N) : (void *)(static_cast<uint16_t *>(y) + (int64_t)m * N);
+    const int nt = n <= 8 ? 1 : n <= 16 ? 2 : 4;
+    const cudaError_t e = nt == 1   ? launch_linear<1, F32>(n, N, K, tiles, xm, ym, st)
+                          : nt == 2 ? launch_linear<2, F32>(n, N, K, tiles, xm, ym, st)
+                                    : launch_linear<4, F32>(n, N, K, tiles, xm, ym, st);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 tq_status linear(int M, int N, int K, const tq_w4_weight *w, const uint16_t *x, void *y, bool f32, void *ws,
@@ -151,9 +402,9 @@ tq_status linear(int M, int N, int K, const tq_w4_weight *w, const uint16_t *x, 
   if (!aligned_to(w->tiles, 16) || !aligned_to(x, 16) || !aligned_to(y, f32 ? 4 : 2) || !aligned_to(ws, 256))
     return TQ_ERR_ALIGN;
   if (ws_bytes < tq_w4_workspace_bytes(M, N, K)) return TQ_ERR_SHAPE;
-  const unsigned grid = (unsigned)(((int64_t)M * N + 7) / 8);
-  return from_cuda(launch_dependent(f32 ? linear_simple_kernel<true> : linear_simple_kernel<false>, dim3(grid), 256,
-                                    (cudaStream_t)stream, M, N, K, w->tiles, x, y));
+  cudaStream_t st = (cudaStream_t)stream;
+  return from_cuda(f32 ? linear_passes<true>(M, N, K, w->tiles, x, y, st)
+                       : linear_passes<false>(M, N, K, w->tiles, x, y, st));
 }
 
 }  // namespace w4
