@@ -151,16 +151,23 @@ __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// The same onto zeros.
+__device__ __forceinline__ void mma_f16_first(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 
 // Shared memory: x in operand order ([group][4][token][4 lanes] 16 bytes), the
 // sums of x per group and token ([group][8 NT] floats), two parts per warp
-// ([16 rows][8 NT] floats each).
+// ([16 rows][8 NT] floats each), 16 zero bytes for the tokens that are not there.
 template <int NT>
 struct Lay {
   static constexpr int kPart = kRows * 8 * NT;  // floats
   static constexpr int kParts = kWarps * 2 * kPart * 4;
   static int64_t bytes(int tokens, int K) {
-    return (int64_t)tokens * K * 2 + (int64_t)(K / kGroup) * 8 * NT * 4 + kParts;
+    return (int64_t)tokens * K * 2 + (int64_t)(K / kGroup) * 8 * NT * 4 + kParts + 16;
   }
 };
 constexpr int kMaxSmem = 232448;
@@ -191,21 +198,27 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int units = (t1 - t0) * G;
   const int each = units / kWarps, more = units % kWarps;
   const int u0 = each * warp + min(warp, more), u1 = u0 + each + (warp < more);
-  const uint8_t *at = tiles + ((int64_t)t0 * G + u0) * kTile + lane * 16;
+  const uint8_t *at = tiles + ((int64_t)t0 * G + u0) * kTile;  // the next unit to be read
+  const int oc = lane * 16, op = kCodes + nr * 4;
   grid_dep_wait();
   Unit q[kAhead];
-  auto load = [&](Unit &v, int u) {
-    if (u < u1) {
-      const uint8_t *p = at + (int64_t)(u - u0) * kTile;
-      v.c0 = ld_stream(p);
-      v.c1 = ld_stream(p + kCodes / 2);
-      const uint32_t *s = reinterpret_cast<const uint32_t *>(p - lane * 16 + kCodes);
-      v.p0 = __ldg(s + nr);
-      v.p1 = __ldg(s + nr + 8);
-    }
+  auto load = [&](Unit &v) {
+    v.c0 = ld_stream(at + oc);
+    v.c1 = ld_stream(at + oc + kCodes / 2);
+    v.p0 = __ldg(reinterpret_cast<const uint32_t *>(at + op));
+    v.p1 = __ldg(reinterpret_cast<const uint32_t *>(at + op + 32));
+    at += kTile;
+  };
+  // A request to L2 for the kAhead units after those just asked for (one
+  // instruction, no registers): with it 131072 x 4096 takes 61 us, without 69.
+  auto prefetch = [&](int u) {
+    const int n = min(kAhead, u1 - u);
+    if (lane == 0 && n > 0)
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(n * kTile));
   };
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) load(q[i], u0 + i);
+  for (int i = 0; i < kAhead; ++i)
+    if (u0 + i < u1) load(q[i]);
   // x: eight threads per (group, token), 16 columns each
   for (int it = tid; it < G * M * 8; it += kThreads) {
     const int part = it & 7, m = (it >> 3) % M, g = (it >> 3) / M, jj = part >> 1, p = part & 1;
@@ -229,6 +242,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(lanes, sum, d);
     if (part == 0) xsum[g * 8 * NT + m] = sum;
   }
+  float *none = parts + Lay<NT>::kParts / 4;
+  if (tid < 4) none[tid] = 0.0f;
   for (int it = tid; it < G * (8 * NT - M); it += kThreads)  // tokens that are not there
     xsum[it / (8 * NT - M) * 8 * NT + M + it % (8 * NT - M)] = 0.0f;
   __syncthreads();
@@ -238,42 +253,38 @@ __global__ void __launch_bounds__(kThreads, 1)
   float Y[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) Y[t][0] = Y[t][1] = Y[t][2] = Y[t][3] = 0.0f;
-  const unsigned char *xl = xs + nr * 64 + j * 16;
-  auto one = [&](Unit &v, int u) {
+  // the lane's operands: token 8 t + nr's, or zeros
+  const unsigned char *xl[NT];
+  int xstep[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const bool there = 8 * t + nr < M;
+    xstep[t] = there ? M * 64 : 0;
+    xl[t] = there ? xs + (8 * t + nr) * 64 + j * 16 + (int64_t)g * 4 * xstep[t] : reinterpret_cast<unsigned char *>(none);
+  }
+  auto one = [&](Unit &v, int u, bool more_units) {
     const uint32_t wa[4] = {v.c0.x, v.c0.y, v.c0.z, v.c0.w}, wb[4] = {v.c1.x, v.c1.y, v.c1.z, v.c1.w};
     const uint32_t p0 = v.p0, p1 = v.p1;
-    load(v, u + kAhead);
+    if (more_units) load(v);
     float acc[NT][4];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
-    const unsigned char *xg = xl + (int64_t)g * 4 * M * 64;
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-#pragma unroll
-      for (int ip = 0; ip < 2; ++ip) {
-        uint4 b[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          b[t] = make_uint4(0, 0, 0, 0);
-          if (8 * t + nr < M) b[t] = *reinterpret_cast<const uint4 *>(xg + (2 * p + ip) * M * 64 + t * 512);
-        }
-        if (ip == 0) {
-          const uint32_t A0[4] = {codes<0>(wa[2 * p]), codes<0>(wb[2 * p]), codes<0>(wa[2 * p + 1]), codes<0>(wb[2 * p + 1])};
-          const uint32_t A1[4] = {codes<1>(wa[2 * p]), codes<1>(wb[2 * p]), codes<1>(wa[2 * p + 1]), codes<1>(wb[2 * p + 1])};
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A0, b[t].x, b[t].y);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A1, b[t].z, b[t].w);
-        } else {
-          const uint32_t A0[4] = {codes<2>(wa[2 * p]), codes<2>(wb[2 * p]), codes<2>(wa[2 * p + 1]), codes<2>(wb[2 * p + 1])};
-          const uint32_t A1[4] = {codes<3>(wa[2 * p]), codes<3>(wb[2 * p]), codes<3>(wa[2 * p + 1]), codes<3>(wb[2 * p + 1])};
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A0, b[t].x, b[t].y);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma_f16(acc[t], A1, b[t].z, b[t].w);
-        }
-      }
-    }
+#define TQ_STEP(I, P, B0, B1, MMA)                                                             \
+  {                                                                                            \
+    const uint32_t A[4] = {codes<I>(wa[2 * P]), codes<I>(wb[2 * P]), codes<I>(wa[2 * P + 1]),  \
+                           codes<I>(wb[2 * P + 1])};                                           \
+    _Pragma("unroll") for (int t = 0; t < NT; ++t) MMA(acc[t], A, b[t].B0, b[t].B1);           \
+  }
+#define TQ_LOAD()                                                                              \
+  _Pragma("unroll") for (int t = 0; t < NT; ++t) {                                             \
+    b[t] = *reinterpret_cast<const uint4 *>(xl[t]);                                            \
+    xl[t] += xstep[t];                                                                         \
+  }
+    uint4 b[NT];
+    TQ_LOAD() TQ_STEP(0, 0, x, y, mma_f16_first) TQ_STEP(1, 0, z, w, mma_f16)
+    TQ_LOAD() TQ_STEP(2, 0, x, y, mma_f16) TQ_STEP(3, 0, z, w, mma_f16)
+    TQ_LOAD() TQ_STEP(0, 1, x, y, mma_f16) TQ_STEP(1, 1, z, w, mma_f16)
+    TQ_LOAD() TQ_STEP(2, 1, x, y, mma_f16) TQ_STEP(3, 1, z, w, mma_f16)
+#undef TQ_STEP
+#undef TQ_LOAD
     const float2 q0 = __half22float2(*reinterpret_cast<const __half2 *>(&p0));
     const float2 q1 = __half22float2(*reinterpret_cast<const __half2 *>(&p1));
     const float m0 = fmaf(8.0f, q0.x, q0.y), m1 = fmaf(8.0f, q1.x, q1.y);
@@ -308,13 +319,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (g == G) {
         g = 0;
         ++tile;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) xl[t] -= (int64_t)G * 4 * xstep[t];
       }
     }
   };
-  for (int u = u0; u < u1; u += kAhead) {
+  int u = u0;
+  for (; u + 2 * kAhead <= u1; u += kAhead) {
+    prefetch(u + kAhead);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) one(q[i], u + i, true);
+  }
+  for (; u < u1; u += kAhead) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (u + i < u1) one(q[i], u + i);
+      if (u + i < u1) one(q[i], u + i, u + i + kAhead < u1);
   }
   __syncthreads();
   // tiles that several warps share
@@ -346,7 +365,7 @@ Pass pass_of(int M, int K) {
     return (int)(room < 8 * nt ? room : 8 * nt);
   };
   const int64_t G = K / kGroup;
-  const int m4 = most(4, Lay<4>::kParts + G * 128), m2 = most(2, Lay<2>::kParts + G * 64), m1 = most(1, Lay<1>::kParts + G * 32);
+  const int m4 = most(4, Lay<4>::kParts + 16 + G * 128), m2 = most(2, Lay<2>::kParts + 16 + G * 64), m1 = most(1, Lay<1>::kParts + 16 + G * 32);
   if (M > 16 && m4 > m2 && m4 > 16) return {4, m4};
   if (M > 8 && m2 > m1) return {2, m2};
   return {1, m1};
