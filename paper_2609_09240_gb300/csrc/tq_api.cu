@@ -50,6 +50,7 @@ cudaError_t read_status_selftest(uint32_t *out, bool clear);
 cudaError_t launch_wait_selftest(int32_t *result, cudaStream_t s);
 namespace kv4 {
 cudaError_t read_status_kv4_attention(uint32_t *out, bool clear);
+cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear);
 }
 }  // namespace tq
 
@@ -624,13 +625,14 @@ tq_status tq_ew_linear_f32out(int32_t M, int32_t N, int32_t K, const tq_ew_weigh
 
 tq_status tq_get_device_status(uint32_t *status_host, int clear) {
   if (!status_host) return TQ_ERR_NULL;
-  uint32_t b = 0, c = 0, d = 0, e = 0, f = 0;
+  uint32_t b = 0, c = 0, d = 0, e = 0, f = 0, g = 0;
   if (read_status_gemv_mma(&b, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (read_status_gemv_g4(&e, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (read_status_prefill(&c, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (read_status_selftest(&d, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
   if (kv4::read_status_kv4_attention(&f, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
-  *status_host = b | c | d | e | f;
+  if (kv4::read_status_kv4_prefill(&g, clear != 0) != cudaSuccess) return TQ_ERR_CUDA;
+  *status_host = b | c | d | e | f | g;
   return TQ_OK;
 }
 

@@ -87,7 +87,7 @@ __device__ __forceinline__ void load_seqs(const AttnArgs &a, int rows_per_tile, 
       T.q0[b] = q0;
       T.L[b] = L;
       T.n[b] = bad ? 0 : n;
-      if (!bad && n > 0) {
+      if (!bad && n > 0 && (int64_t)n * g < a.many_rows) {
         int p0, np;
         seq_pages(a, L, n, &p0, &np);
         const int tiles = (int)(((int64_t)n * g + rows_per_tile - 1) / rows_per_tile);
@@ -824,6 +824,10 @@ inline size_t split_ws_bytes(int D, int NT) {
   const int warps = NT == 1 ? Shape<128, 1>::kWarps : Shape<128, 2>::kWarps;
   return (size_t)sm_count() * warps * (sizeof(Join) + 2 * (8 * NT) * (D + 2) * 4);
 }
+#ifndef MANY
+#define MANY 64
+#endif
+constexpr int kManyRows = MANY;
 inline int split_tiles(int max_q, int group) { return (int64_t)max_q * group <= 8 ? 1 : 2; }
 
 template <int D, int NT, bool BF16>
@@ -889,12 +893,18 @@ tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t count, 
     return TQ_ERR_ALIGN;
   if (workspace_bytes < tq_kv4_attention_workspace_bytes(c, count, tokens, max_q, q_heads)) return TQ_ERR_SHAPE;
   if (tokens == 0) return TQ_OK;
-  const AttnArgs a = {*c,  layer,    count,      tokens, q_heads, causal != 0, window, slots, indptr, q, out, lse,
-                      q_stride, out_stride, scale,  d_status};
+  const int g = q_heads / c->heads;
+  const bool many = (int64_t)max_q * g >= kManyRows, bf16 = dtype == TQ_BF16;
+  const AttnArgs a = {*c,  layer,    count,      tokens, q_heads, causal != 0,                     window, slots, indptr, q, out, lse,
+                      q_stride, out_stride, scale,  d_status, many ? kManyRows : 0x7fffffff};
   cudaStream_t st = (cudaStream_t)stream;
-  const int nt = split_tiles(max_q, q_heads / c->heads);
-  return from_cuda(c->dim == 128 ? split_attention<128>(a, nt, dtype == TQ_BF16, workspace, st)
-                                 : split_attention<64>(a, nt, dtype == TQ_BF16, workspace, st));
+  if (many) {
+    const cudaError_t e = launch_attn_prefill(a, bf16, st);
+    if (e != cudaSuccess) return TQ_ERR_CUDA;
+  }
+  const int nt = split_tiles(max_q, g);
+  return from_cuda(c->dim == 128 ? split_attention<128>(a, nt, bf16, workspace, st)
+                                 : split_attention<64>(a, nt, bf16, workspace, st));
 }
 
 }  // extern "C"

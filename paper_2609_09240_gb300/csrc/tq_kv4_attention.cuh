@@ -16,7 +16,12 @@ struct AttnArgs {
   int64_t q_stride, out_stride;
   float scale;
   uint32_t *d_status;
+  // sequences with this many query rows per K/V head or more are the kernel's
+  // for many rows (tq_kv4_prefill.cu)
+  int32_t many_rows;
 };
+cudaError_t launch_attn_prefill(const AttnArgs &a, bool bf16, cudaStream_t st);
+cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear);
 
 // Two results in the output's type.
 template <bool BF16>

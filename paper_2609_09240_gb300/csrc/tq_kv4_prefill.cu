@@ -1,0 +1,552 @@
+// tq_kv4_prefill.cu - attention over the 4-bit K/V cache for many query rows
+// (prompts in pieces): keys and values are decoded to fp16 tiles in shared
+// memory and multiplied by tcgen05 MMAs.
+//
+// Mathematics.  s (c - z) of the cache is an fp16 number (seven bits times four), so
+// the decoded tiles are exact: (1024 + c) - (1024 + z), times s, each one packed
+// instruction.  S = Q K^T and O += P V accumulate in fp32 in tensor memory, the
+// softmax's maximum and sum are fp32 registers of the thread that owns the row;
+// P is rounded to fp16, once.  The reference of the exponentials follows the
+// running maximum only when that has grown by a factor of 2^8: O is rescaled a few
+// times in a long sequence, not once a tile.  P counts 2^7 where the score is the
+// reference, so it stays below 2^15, and rounds as a normal number down to 2^-21.
+//
+// A block (one per SM) takes 256 query rows of one K/V head (a row is a query
+// token and one of the head's query heads) in two tiles of 128, and walks over
+// the keys 128 tokens (two pages) at a time:
+//   warps 0..3, 4..7   softmax of tile 0 and 1, a row per thread: S from tensor
+//                      memory, P back over it
+//   warps 8..15        decode K and V tiles (two stages each) for both tiles
+//   warp 16            one thread issues the MMAs: while one tile's softmax runs
+//                      the tensor cores work for the other
+// Tensor memory: S (P in its first half) of both tiles 2 x 128 columns, O 2 x D.
+// K tiles are K-major, V tiles the same bytes read MN-major (tokens are the
+// contraction there), in core matrices of 8 tokens x 16 bytes, unswizzled.  The
+// dimensions of a code word decode in the order 0 4 1 5 2 6 3 7; Q is stored in
+// that order and O read back from it.
+#include <cmath>
+#include <limits>
+
+#include "tq_kv4_attention.cuh"
+#include "tq_launch.cuh"
+#include "tq_sm100.cuh"
+
+namespace tq {
+namespace kv4 {
+namespace pf {
+
+constexpr int kTile = 128;                   // tokens of a K/V tile, rows of a row tile
+constexpr int kSoftWarps = 8, kDecWarps = 8, kMmaWarp = 16;
+constexpr int kThreads = 17 * 32;
+constexpr int kDecThreads = kDecWarps * 32;
+constexpr float kInf = std::numeric_limits<float>::infinity();
+constexpr float kGrow = 8.0f, kUp = 7.0f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <int D>
+struct Lay {
+  static constexpr int kChunks = D / 8;              // 16-byte pieces of a row
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int oQ = 0;                       // two row tiles
+  static constexpr int oK = 2 * kTileBytes;          // two stages
+  static constexpr int oV = oK + 2 * kTileBytes;
+  static constexpr int oLost = oV + 2 * kTileBytes;  // of four tiles, per group and octet: tokens that stand for NaN
+  static constexpr int oBar = oLost + 4 * (D / kGrp) * 16;
+  static constexpr int kSmem = oBar + 256;
+  static_assert(kSmem <= 232448, "shared memory");
+};
+struct Bars {
+  uint64_t q, kfull[2], kempty[2], vfull[2], vempty[2], s[2], p[2], o[2];
+  uint32_t tmem;
+  int32_t abort_;
+};
+static_assert(sizeof(Bars) <= 256, "barriers");
+
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, volatile int32_t *abort_) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (mbar_try_wait_sleep(bar, parity, 20000u)) return true;
+    if ((i & 7u) == 0) {
+      if (*abort_) return false;
+      if (global_ns() - t0 > kWaitLimitNs) break;
+    }
+  }
+  atomicOr(&g_tq_device_status, kStatusTimeout);
+  *abort_ = 1;
+  return false;
+}
+
+// 32 columns of the warp's 32 lanes.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
+__device__ __forceinline__ uint32_t as_bits(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
+
+// The eight values of a code word, dimensions 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ uint4 decode(uint32_t w, __half2 s, __half2 za, __half2 zb) {
+  const uint32_t v = w >> 8;
+  return make_uint4(as_bits(__hmul2(__hsub2(as_half2(and_or(w, 0x000F000Fu, 0x64006400u)), za), s)),
+                    as_bits(__hmul2(__hsub2(as_half2(and_or(w, 0x00F000F0u, 0x54005400u)), zb), s)),
+                    as_bits(__hmul2(__hsub2(as_half2(and_or(v, 0x000F000Fu, 0x64006400u)), za), s)),
+                    as_bits(__hmul2(__hsub2(as_half2(and_or(v, 0x00F000F0u, 0x54005400u)), zb), s)));
+}
+
+// What a block works on.
+struct Task {
+  int b, h, row0, rows;      // sequence, head, first row, rows from there on (<= 256)
+  int L, n, q0, slot;
+  int t0, tiles[2];          // first token; K/V tiles of each row tile
+};
+
+// One block: 256 rows.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArgs a) {
+  using B = Block<D>;
+  using Y = Lay<D>;
+  constexpr int G = B::kGroups, C = Y::kChunks;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ Task T;
+  Bars *bars = reinterpret_cast<Bars *>(smem + Y::oBar);
+  volatile int32_t *abort_ = &bars->abort_;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = a.q_heads / a.c.heads;
+  if (tid == 0) {
+    mbar_init(&bars->q, kSoftWarps * 32);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->kfull[i], kDecThreads);
+      mbar_init(&bars->vfull[i], kDecThreads);
+      mbar_init(&bars->kempty[i], 1);
+      mbar_init(&bars->vempty[i], 1);
+      mbar_init(&bars->s[i], 1);
+      mbar_init(&bars->p[i], 128);
+      mbar_init(&bars->o[i], 1);
+    }
+    bars->abort_ = 0;
+    mbar_fence_init();
+  }
+  grid_dep_wait();
+  // ---- the block's task: sequences' row tiles one after another, the last
+  // (longest) first; heads side by side, they share the table
+  if (warp == 0) {
+    const int h = blockIdx.x % a.c.heads;
+    int64_t want = blockIdx.x / a.c.heads;
+    int found = -1, n_ = 0, q0_ = 0;
+    for (int base = 0; base < a.count && found < 0; base += 32) {
+      const int b = base + lane;
+      int n = 0, q0 = 0;
+      if (b < a.count) {
+        q0 = a.indptr[b];
+        n = a.indptr[b + 1] - q0;
+        if (q0 < 0 || n < 0 || n > a.tokens - q0) n = 0;  // reported by the other kernel
+        if ((int64_t)n * g < a.many_rows) n = 0;          // that kernel's
+      }
+      const int tiles = (int)(((int64_t)n * g + 2 * kTile - 1) / (2 * kTile));
+      int x = tiles;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      const uint32_t hit = __ballot_sync(0xffffffffu, want < x);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        found = base + l;
+        const int last = __shfl_sync(0xffffffffu, x, l);
+        n_ = __shfl_sync(0xffffffffu, n, l);
+        q0_ = __shfl_sync(0xffffffffu, q0, l);
+        want = (last - 1) - want;  // within the sequence, from its end
+      } else {
+        want -= __shfl_sync(0xffffffffu, x, 31);
+      }
+    }
+    if (lane == 0) {
+      T.b = found;
+      if (found >= 0) {
+        const int slot = a.slots[found];
+        int L = slot >= 0 && slot < a.c.slots ? a.c.length[slot] : -1;
+        if (L != clamp_length(a.c, L) || L < 0) {
+          T.b = -1;  // reported by the other kernel
+        } else {
+          T.h = h;
+          T.slot = slot;
+          T.L = L;
+          T.n = n_;
+          T.q0 = q0_;
+          T.row0 = (int)want * 2 * kTile;
+          T.rows = min(n_ * g - T.row0, 2 * kTile);
+          const int first = L - n_ + T.row0 / g;  // position of the first row
+          T.t0 = a.window > 0 ? max(0, first - a.window + 1) / kPage * kPage : 0;
+          for (int i = 0; i < 2; ++i) {
+            const int r = min(T.rows, (i + 1) * kTile) - 1;  // the row tile's last row
+            int end = r < i * kTile ? 0 : a.causal ? L - n_ + (T.row0 + r) / g + 1 : L;
+            T.tiles[i] = end > T.t0 ? (end - T.t0 + kTile - 1) / kTile : 0;
+          }
+        }
+      }
+    }
+  }
+  if (warp == kMmaWarp) tmem_alloc(&bars->tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem;
+  const bool work = T.b >= 0;
+  const int tiles = work ? max(T.tiles[0], T.tiles[1]) : 0;
+
+  if (work && warp < kSoftWarps) {
+    // ======================================================== softmax, a row per thread
+    const int i = warp >> 2, r = tid & 127;  // row tile and row
+    const int row = T.row0 + i * kTile + r;
+    const bool there = i * kTile + r < T.rows;
+    const int64_t token = T.q0 + (there ? row / g : 0);
+    const int head = T.h * g + (there ? row % g : 0);
+    // ---- Q: fp16, in the decoding's order of dimensions
+    float F = 1.0f;
+    {
+      const uint4 *src = reinterpret_cast<const uint4 *>(a.q + token * a.q_stride + head * D);
+      unsigned char *dst = smem + Y::oQ + i * Y::kTileBytes + ((r >> 3) * C) * 128 + (r & 7) * 16;
+      float up = 1.0f;
+      int e = 0;
+      if (BF16) {  // a power of two brings the row's largest value into [2^10, 2^11)
+        float top = 0.0f;
+        if (there)
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const uint4 v = __ldg(src + c);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xFFFF0000u))));
+          }
+        if (top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
+        up = __uint_as_float((uint32_t)(127 + e) << 23);
+      }
+      // a negative scale turns the queries' sign, none makes them zeros: F > 0
+      up = a.scale < 0.0f ? -up : a.scale == 0.0f ? 0.0f : up;
+      if (a.scale != 0.0f) F = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-37f);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const uint4 v = there ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          f[2 * k] = BF16 ? __uint_as_float(w[k] << 16) : __half2float(__ushort_as_half((uint16_t)w[k]));
+          f[2 * k + 1] =
+              BF16 ? __uint_as_float(w[k] & 0xFFFF0000u) : __half2float(__ushort_as_half((uint16_t)(w[k] >> 16)));
+        }
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = pack_out<false>(f[k] * up, f[4 + k] * up);
+        *reinterpret_cast<uint4 *>(dst + c * 128) = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+    }
+    fence_proxy_async_smem();
+    mbar_arrive(&bars->q);
+    // ---- what the row sees: [begin, end)
+    const int pos = T.L - T.n + row / g;
+    const int end = !there ? 0 : a.causal ? pos + 1 : T.L, begin = a.window > 0 ? pos - a.window + 1 : 0;
+    // what every row of the tile sees
+    const int pos_lo = T.L - T.n + (T.row0 + i * kTile) / g;
+    const int pos_hi = T.L - T.n + (T.row0 + min(T.rows, (i + 1) * kTile) - 1) / g;
+    const int all_end = a.causal ? pos_lo + 1 : T.L, all_begin = a.window > 0 ? pos_hi - a.window + 1 : 0;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 (warp % 4) in the lane field
+    const uint32_t tS = tmem + i * kTile + lanes, tO = tmem + 2 * kTile + i * D + lanes;
+    float m = -kInf, l = 0.0f;  // the reference of the exponentials (a score before F) and the sum
+    uint32_t lost = 0;          // groups with a NaN that the row sees
+    const int n = T.tiles[i];
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      if (!__all_sync(0xffffffffu, wait(&bars->s[i], j & 1, abort_))) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const int tok = T.t0 + j * kTile;
+      const bool plain = tok >= all_begin && tok + kTile <= all_end;
+      // the columns that the row sees
+      const int lo = max(begin - tok, 0), hi = min(end - tok, kTile);
+      float x[32], top = -kInf;
+#pragma unroll
+      for (int c = 0; c < kTile / 32; ++c) {
+        tmem_ld32(tS + 32 * c, reinterpret_cast<uint32_t *>(x));
+        tmem_wait_ld();
+        if (plain) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) top = fmaxf(top, x[k]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (32 * c + k >= lo && 32 * c + k < hi) top = fmaxf(top, x[k]);
+        }
+      }
+      // rows whose maximum has grown by more than 2^8 take it as their reference
+      const bool grow = top > m && (m == -kInf || (top - m) * F > kGrow);
+      if (__any_sync(0xffffffffu, grow && m != -kInf)) {
+        const float f = grow && m != -kInf ? exp2_fast((m - top) * F) : 1.0f;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          tmem_ld32(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] *= f;
+          tmem_st16(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
+          tmem_st16(tO + 32 * c + 16, reinterpret_cast<uint32_t *>(x) + 16);
+        }
+      }
+      if (grow) m = top;
+      const float ref = m == -kInf ? 0.0f : m * F - kUp;
+      // tokens that stand for NaN in V were decoded as zeros
+      {
+        const uint4 *v = reinterpret_cast<const uint4 *>(smem + Y::oLost + (j & 3) * G * 16);
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr) {
+          const uint4 w = v[gr];
+          if (w.x | w.y | w.z | w.w) {
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+            for (int k = lo; k < hi; ++k)
+              if (ws[k >> 5] >> (k & 31) & 1) lost |= 1u << gr;
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < kTile / 32; ++c) {
+        tmem_ld32(tS + 32 * c, reinterpret_cast<uint32_t *>(x));
+        tmem_wait_ld();
+        uint32_t p[16];
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          float p0 = x[2 * k], p1 = x[2 * k + 1];
+          if (!plain) {
+            if (32 * c + 2 * k < lo || 32 * c + 2 * k >= hi) p0 = -kInf;
+            if (32 * c + 2 * k + 1 < lo || 32 * c + 2 * k + 1 >= hi) p1 = -kInf;
+          }
+          p0 = exp2_fast(fmaf(p0, F, -ref));
+          p1 = exp2_fast(fmaf(p1, F, -ref));
+          s0 += p0;
+          s1 += p1;
+          p[k] = pack_out<false>(p0, p1);
+        }
+        l += s0 + s1;
+        tmem_st16(tS + 16 * c, p);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(&bars->p[i]);
+    }
+    // ---- the result
+    if (n > 0 && ok) ok = __all_sync(0xffffffffu, wait(&bars->o[i], 0, abort_));
+    if (ok) {
+      tc_fence_after();
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      uint16_t *out = a.out + token * a.out_stride + head * D;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        float x[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) x[k] = 0.0f;
+        if (n > 0) {
+          tmem_ld32(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
+          tmem_wait_ld();
+        }
+        const bool nan = lost >> (32 * c / kGrp) & 1;
+        if (there)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              f[k] = nan ? kInf - kInf : l == 0.0f ? 0.0f : x[8 * q + (k < 4 ? 2 * k : 2 * k - 7)] * inv;
+            *reinterpret_cast<uint4 *>(out + 32 * c + 8 * q) =
+                make_uint4(pack_out<BF16>(f[0], f[1]), pack_out<BF16>(f[2], f[3]), pack_out<BF16>(f[4], f[5]),
+                           pack_out<BF16>(f[6], f[7]));
+          }
+      }
+      if (there && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -kInf : kLn2 * (m * F - kUp + log2f(l));
+    }
+    tc_fence_before();
+  } else if (work && warp < kSoftWarps + kDecWarps) {
+    // ======================================================== decode
+    // A lane takes 16 bytes of codes (32 dimensions) of a token; eight tokens side
+    // by side fill a core matrix.
+    constexpr int Q = D / 32, ITEMS = kTile * Q / kDecThreads, OPW = 4 / Q;  // octets that a warp covers at once
+    const int dw = warp - kSoftWarps, q = (lane >> 3) % Q;
+    int octet[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) octet[k] = (dw + k * kDecWarps) * OPW + (lane >> 3) / Q;
+    const int gr = q * 32 / kGrp;
+    const int32_t *table = a.c.table + (int64_t)T.slot * a.c.max_pages;
+    const int pages = (T.L + kPage - 1) / kPage;
+    struct Raw {
+      uint4 k, v;
+      uint32_t pk, pv;
+    } raw[ITEMS];
+    auto page_of = [&](int j, int k) {  // -1: nothing there
+      const int pg = (T.t0 + j * kTile + octet[k] * 8) / kPage;
+      if (j >= tiles || pg >= pages) return -1;
+      const int p = table[pg];
+      if (p >= 0 && p < a.c.pages) return p;
+      report(a.d_status, TQ_DATA_BAD_SLOT);
+      return -1;
+    };
+    int page[ITEMS];
+    auto load = [&](int j) {
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        Raw &w = raw[k];
+        w.k = w.v = make_uint4(0, 0, 0, 0);
+        w.pk = w.pv = 0;
+        const int tok = T.t0 + j * kTile + octet[k] * 8 + (lane & 7), off = tok & (kPage - 1);
+        if (page[k] >= 0 && tok < T.L) {
+          const uint8_t *blk = a.c.data + (((int64_t)a.layer * a.c.pages + page[k]) * a.c.heads + T.h) * B::kBytes;
+          w.k = __ldg(reinterpret_cast<const uint4 *>(blk + B::oK + off * B::kRow + q * 16));
+          w.v = __ldg(reinterpret_cast<const uint4 *>(blk + B::oV + off * B::kRow + q * 16));
+          w.pk = __ldg(reinterpret_cast<const uint16_t *>(blk + B::oPK + (gr * kPage + off) * 2));
+          w.pv = __ldg(reinterpret_cast<const uint16_t *>(blk + B::oPV + (gr * kPage + off) * 2));
+        }
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) page[k] = page_of(0, k);
+    load(0);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) page[k] = page_of(1, k);
+    auto put = [&](unsigned char *tile, int k, const uint4 &codes, uint32_t param) {
+      const uint32_t z = (param & 15u) * 0x10001u;
+      const __half2 za = as_half2(z | 0x64006400u), zb = as_half2(z << 4 | 0x54005400u);
+      const __half2 s = as_half2((param & 0xFFF0u) * 0x10001u);
+      unsigned char *dst = tile + (octet[k] * C + 4 * q) * 128 + (lane & 7) * 16;
+      *reinterpret_cast<uint4 *>(dst) = decode(codes.x, s, za, zb);
+      *reinterpret_cast<uint4 *>(dst + 128) = decode(codes.y, s, za, zb);
+      *reinterpret_cast<uint4 *>(dst + 256) = decode(codes.z, s, za, zb);
+      *reinterpret_cast<uint4 *>(dst + 384) = decode(codes.w, s, za, zb);
+    };
+    for (int j = 0; j < tiles; ++j) {
+      const int st = j & 1;
+      Raw cur[ITEMS];
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) cur[k] = raw[k];
+      if (j + 1 < tiles) {
+        load(j + 1);
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) page[k] = page_of(j + 2, k);
+      }
+      if (j >= 2 && !__all_sync(0xffffffffu, wait(&bars->kempty[st], ((j >> 1) & 1) ^ 1, abort_))) break;
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        put(smem + Y::oK + st * Y::kTileBytes, k, cur[k].k, cur[k].pk);
+        // Values that stand for NaN become zeros (0 times NaN must not count) and are noted for
+        // the rows that see them, with the tile's scores.  Four tiles' notes: the values of the
+        // tile before this one went to a stage whose tile, three before, every row was done with.
+        const uint32_t bits = __ballot_sync(0xffffffffu, (cur[k].pv & 0x7C00u) == 0x7C00u);
+        if ((lane & 7) == 0 && q * 32 % kGrp == 0)
+          smem[Y::oLost + ((j & 3) * G + gr) * 16 + octet[k]] = (unsigned char)(bits >> lane);
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&bars->kfull[st]);
+      if (j >= 2 && !__all_sync(0xffffffffu, wait(&bars->vempty[st], ((j >> 1) & 1) ^ 1, abort_))) break;
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        const bool nan = (cur[k].pv & 0x7C00u) == 0x7C00u;
+        put(smem + Y::oV + st * Y::kTileBytes, k, cur[k].v, nan ? 0u : cur[k].pv);
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&bars->vfull[st]);
+    }
+  } else if (work && warp == kMmaWarp && lane == 0 && tiles > 0) {
+    // ======================================================== MMA
+    const uint32_t idS = idesc_f16_f32(kTile, kTile), idO = idesc_f16_f32(kTile, D) | (1u << 16);  // V: MN-major
+    const uint32_t sQ = smem_u32(smem + Y::oQ), sK = smem_u32(smem + Y::oK), sV = smem_u32(smem + Y::oV);
+    auto scores = [&](int i, int st) {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        mma_smemA(tmem + i * kTile, smem_desc(sQ + i * Y::kTileBytes + k * 256, 128, C * 128),
+                  smem_desc(sK + st * Y::kTileBytes + k * 256, 128, C * 128), idS, k > 0);
+      mma_commit(&bars->s[i]);
+    };
+    auto values = [&](int i, int j) {
+#pragma unroll
+      for (int k = 0; k < kTile / 16; ++k)
+        mma_tmemA(tmem + 2 * kTile + i * D, tmem + i * kTile + k * 8,
+                  smem_desc(sV + (j & 1) * Y::kTileBytes + k * 2 * C * 128, C * 128, 128), idO, j > 0 || k > 0);
+    };
+    const int n0 = T.tiles[0], n1 = T.tiles[1];
+    bool ok = wait(&bars->q, 0, abort_) && wait(&bars->kfull[0], 0, abort_);
+    if (ok) {
+      tc_fence_after();
+      if (n0 > 0) scores(0, 0);
+      if (n1 > 0) scores(1, 0);
+      mma_commit(&bars->kempty[0]);
+    }
+    for (int j = 0; j < tiles && ok; ++j) {
+      const int st = j & 1, nx = (j + 1) & 1;
+      if (!(ok = wait(&bars->vfull[st], (j >> 1) & 1, abort_))) break;
+      for (int i = 0; i < 2 && ok; ++i) {
+        const int n = i ? n1 : n0;
+        if (j < n) {
+          if (!(ok = wait(&bars->p[i], j & 1, abort_))) break;
+          tc_fence_after();
+          values(i, j);
+          if (j + 1 == n) mma_commit(&bars->o[i]);
+        }
+        if (i == 1) mma_commit(&bars->vempty[st]);
+        if (j + 1 < tiles) {
+          if (i == 0 && !(ok = wait(&bars->kfull[nx], ((j + 1) >> 1) & 1, abort_))) break;
+          tc_fence_after();
+          if (j + 1 < n) scores(i, nx);
+          if (i == 1) mma_commit(&bars->kempty[nx]);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+TQ_STATUS_ACCESSOR(read_status_impl)
+
+}  // namespace pf
+
+cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear) { return pf::read_status_impl(out, clear); }
+
+// The sequences with at least a.many_rows query rows per K/V head.
+cudaError_t launch_attn_prefill(const AttnArgs &a, bool bf16, cudaStream_t st) {
+  const int g = a.q_heads / a.c.heads;
+  const int64_t blocks = ((int64_t)a.tokens * g / (2 * pf::kTile) + a.count) * a.c.heads;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  auto go = [&](auto kern, int smem) {
+    return launch_big_smem(kern, (int)blocks, pf::kThreads, smem, st, a);
+  };
+  if (a.c.dim == 128)
+    return bf16 ? go(pf::attn_prefill_kernel<128, true>, pf::Lay<128>::kSmem)
+                : go(pf::attn_prefill_kernel<128, false>, pf::Lay<128>::kSmem);
+  return bf16 ? go(pf::attn_prefill_kernel<64, true>, pf::Lay<64>::kSmem)
+              : go(pf::attn_prefill_kernel<64, false>, pf::Lay<64>::kSmem);
+}
+
+}  // namespace kv4
+}  // namespace tq
