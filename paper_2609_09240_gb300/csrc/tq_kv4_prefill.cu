@@ -37,7 +37,7 @@ namespace pf {
 
 constexpr int kTile = 128;                   // tokens of a K/V tile, rows of a row tile
 constexpr int kSoftWarps = 8, kDecWarps = 8, kMmaWarp = 16;
-constexpr int kThreads = 17 * 32;
+constexpr int kThreads = 20 * 32;  // five warpgroups, for their register counts
 constexpr int kDecThreads = kDecWarps * 32;
 constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr float kGrow = 8.0f, kUp = 7.0f;
@@ -88,6 +88,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr)
       : "memory");
+}
+// The warpgroup's registers per thread from here on.  640 threads are launched
+// with 96 each; 256 x 144 + 256 x 64 + 128 x 64 are as many.
+template <int N>
+__device__ __forceinline__ void registers_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void registers_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -210,6 +220,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem;
+  if (warp < kSoftWarps)
+    registers_up<144>();
+  else
+    registers_down<64>();
   const bool work = T.b >= 0;
   const int tiles = work ? max(T.tiles[0], T.tiles[1]) : 0;
 
@@ -286,33 +300,36 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       const bool plain = tok >= all_begin && tok + kTile <= all_end;
       // the columns that the row sees
       const int lo = max(begin - tok, 0), hi = min(end - tok, kTile);
-      float x[32], top = -kInf;
-#pragma unroll
-      for (int c = 0; c < kTile / 32; ++c) {
+      // the columns 32 c .. 32 c + 31, what is not seen at -inf
+      auto load = [&](int c, float *x) {
         tmem_ld32(tS + 32 * c, reinterpret_cast<uint32_t *>(x));
         tmem_wait_ld();
-        if (plain) {
-#pragma unroll
-          for (int k = 0; k < 32; ++k) top = fmaxf(top, x[k]);
-        } else {
+        if (!plain) {
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (32 * c + k >= lo && 32 * c + k < hi) top = fmaxf(top, x[k]);
+            if (32 * c + k < lo || 32 * c + k >= hi) x[k] = -kInf;
         }
+      };
+      float x[32], top = -kInf;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        load(c, x);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) top = fmaxf(top, x[k]);
       }
       // rows whose maximum has grown by more than 2^8 take it as their reference
       const bool grow = top > m && (m == -kInf || (top - m) * F > kGrow);
       if (__any_sync(0xffffffffu, grow && m != -kInf)) {
         const float f = grow && m != -kInf ? exp2_fast((m - top) * F) : 1.0f;
         l *= f;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          tmem_ld32(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t o[16];
+          tmem_ld_cols<16>(tO + 16 * c, o);
           tmem_wait_ld();
 #pragma unroll
-          for (int k = 0; k < 32; ++k) x[k] *= f;
-          tmem_st16(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
-          tmem_st16(tO + 32 * c + 16, reinterpret_cast<uint32_t *>(x) + 16);
+          for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+          tmem_st16(tO + 16 * c, o);
         }
       }
       if (grow) m = top;
@@ -330,28 +347,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
           }
         }
       }
+      // P over the first half of S, in order: its piece c lies on what pieces 0 .. c / 2 were
+      float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-      for (int c = 0; c < kTile / 32; ++c) {
-        tmem_ld32(tS + 32 * c, reinterpret_cast<uint32_t *>(x));
-        tmem_wait_ld();
+      for (int c = 0; c < 4; ++c) {
+        load(c, x);  // again: the registers do not hold the whole row
         uint32_t p[16];
-        float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-          float p0 = x[2 * k], p1 = x[2 * k + 1];
-          if (!plain) {
-            if (32 * c + 2 * k < lo || 32 * c + 2 * k >= hi) p0 = -kInf;
-            if (32 * c + 2 * k + 1 < lo || 32 * c + 2 * k + 1 >= hi) p1 = -kInf;
-          }
-          p0 = exp2_fast(fmaf(p0, F, -ref));
-          p1 = exp2_fast(fmaf(p1, F, -ref));
+          const float p0 = exp2_fast(fmaf(x[2 * k], F, -ref));
+          const float p1 = exp2_fast(fmaf(x[2 * k + 1], F, -ref));
           s0 += p0;
           s1 += p1;
           p[k] = pack_out<false>(p0, p1);
         }
-        l += s0 + s1;
         tmem_st16(tS + 16 * c, p);
       }
+      l += s0 + s1;
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(&bars->p[i]);
@@ -480,14 +492,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
     const uint32_t idS = idesc_f16_f32(kTile, kTile), idO = idesc_f16_f32(kTile, D) | (1u << 16);  // V: MN-major
     const uint32_t sQ = smem_u32(smem + Y::oQ), sK = smem_u32(smem + Y::oK), sV = smem_u32(smem + Y::oV);
     auto scores = [&](int i, int st) {
-#pragma unroll
+#pragma unroll 1
       for (int k = 0; k < D / 16; ++k)
         mma_smemA(tmem + i * kTile, smem_desc(sQ + i * Y::kTileBytes + k * 256, 128, C * 128),
                   smem_desc(sK + st * Y::kTileBytes + k * 256, 128, C * 128), idS, k > 0);
       mma_commit(&bars->s[i]);
     };
     auto values = [&](int i, int j) {
-#pragma unroll
+#pragma unroll 1
       for (int k = 0; k < kTile / 16; ++k)
         mma_tmemA(tmem + 2 * kTile + i * D, tmem + i * kTile + k * 8,
                   smem_desc(sV + (j & 1) * Y::kTileBytes + k * 2 * C * 128, C * 128, 128), idO, j > 0 || k > 0);
