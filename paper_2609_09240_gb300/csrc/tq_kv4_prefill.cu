@@ -89,8 +89,25 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
       : "r"(taddr)
       : "memory");
 }
+// Waits for the thread's loads; the registers are named so that no use of them
+// moves ahead of it.
+__device__ __forceinline__ void tmem_wait32(uint32_t *r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                 "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31])::"memory");
+}
 // The warpgroup's registers per thread from here on.  640 threads are launched
-// with 96 each; 256 x 144 + 256 x 64 + 128 x 64 are as many.
+// with 96 each; what the warpgroups take is no more.
+#ifndef SR
+#define SR 160
+#define DR 56
+#define MR 48
+#endif
+constexpr int kSoftRegs = SR, kDecRegs = DR, kMmaRegs = MR;
+static_assert(256 * kSoftRegs + 256 * kDecRegs + 128 * kMmaRegs <= kThreads * 96, "registers of the launch");
 template <int N>
 __device__ __forceinline__ void registers_up() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -220,14 +237,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem;
-  if (warp < kSoftWarps)
-    registers_up<144>();
-  else
-    registers_down<64>();
   const bool work = T.b >= 0;
   const int tiles = work ? max(T.tiles[0], T.tiles[1]) : 0;
 
-  if (work && warp < kSoftWarps) {
+  // (a block without work has no tiles and no rows: every role falls through)
+  if (warp < kSoftWarps) {
+    registers_up<kSoftRegs>();
+    if (work) {
     // ======================================================== softmax, a row per thread
     const int i = warp >> 2, r = tid & 127;  // row tile and row
     const int row = T.row0 + i * kTile + r;
@@ -300,23 +316,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       const bool plain = tok >= all_begin && tok + kTile <= all_end;
       // the columns that the row sees
       const int lo = max(begin - tok, 0), hi = min(end - tok, kTile);
-      // the columns 32 c .. 32 c + 31, what is not seen at -inf
-      auto load = [&](int c, float *x) {
-        tmem_ld32(tS + 32 * c, reinterpret_cast<uint32_t *>(x));
-        tmem_wait_ld();
-        if (!plain) {
+      // columns 32 c .. 32 c + 31: what is not seen at -inf
+      auto hide = [&](int c, uint32_t *x) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (32 * c + k < lo || 32 * c + k >= hi) x[k] = -kInf;
-        }
+        for (int k = 0; k < 32; ++k)
+          if (32 * c + k < lo || 32 * c + k >= hi) x[k] = 0xFF800000u;
       };
-      float x[32], top = -kInf;
+      uint32_t x[2][32];  // a piece at hand, the next one on its way
+      float top4[4] = {-kInf, -kInf, -kInf, -kInf};
+      tmem_ld32(tS, x[0]);
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        load(c, x);
+        tmem_wait32(x[c & 1]);
+        tmem_ld32(tS + 32 * ((c + 1) & 3), x[(c + 1) & 1]);  // at last the first one again
+        if (!plain) hide(c, x[c & 1]);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) top = fmaxf(top, x[k]);
+        for (int k = 0; k < 32; ++k) top4[k & 3] = fmaxf(top4[k & 3], __uint_as_float(x[c & 1][k]));
       }
+      const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
       // rows whose maximum has grown by more than 2^8 take it as their reference
       const bool grow = top > m && (m == -kInf || (top - m) * F > kGrow);
       if (__any_sync(0xffffffffu, grow && m != -kInf)) {
@@ -336,34 +353,35 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       const float ref = m == -kInf ? 0.0f : m * F - kUp;
       // tokens that stand for NaN in V were decoded as zeros
       {
-        const uint4 *v = reinterpret_cast<const uint4 *>(smem + Y::oLost + (j & 3) * G * 16);
+        const uint32_t *notes = reinterpret_cast<const uint32_t *>(smem + Y::oLost + (j & 3) * G * 16);
+        uint32_t any = 0;
 #pragma unroll
-        for (int gr = 0; gr < G; ++gr) {
-          const uint4 w = v[gr];
-          if (w.x | w.y | w.z | w.w) {
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-            for (int k = lo; k < hi; ++k)
-              if (ws[k >> 5] >> (k & 31) & 1) lost |= 1u << gr;
-          }
-        }
+        for (int k = 0; k < 4 * G; ++k) any |= notes[k];
+        if (any)
+#pragma unroll 1
+          for (int k = lo; k < hi; ++k)
+#pragma unroll
+            for (int gr = 0; gr < G; ++gr) lost |= (notes[4 * gr + (k >> 5)] >> (k & 31) & 1u) << gr;
       }
       // P over the first half of S, in order: its piece c lies on what pieces 0 .. c / 2 were
-      float s0 = 0.0f, s1 = 0.0f;
+      float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        load(c, x);  // again: the registers do not hold the whole row
+        tmem_wait32(x[c & 1]);
+        if (c < 3) tmem_ld32(tS + 32 * (c + 1), x[(c + 1) & 1]);
+        if (!plain) hide(c, x[c & 1]);
         uint32_t p[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-          const float p0 = exp2_fast(fmaf(x[2 * k], F, -ref));
-          const float p1 = exp2_fast(fmaf(x[2 * k + 1], F, -ref));
-          s0 += p0;
-          s1 += p1;
+          const float p0 = exp2_fast(fmaf(__uint_as_float(x[c & 1][2 * k]), F, -ref));
+          const float p1 = exp2_fast(fmaf(__uint_as_float(x[c & 1][2 * k + 1]), F, -ref));
+          s4[2 * (k & 1)] += p0;
+          s4[2 * (k & 1) + 1] += p1;
           p[k] = pack_out<false>(p0, p1);
         }
         tmem_st16(tS + 16 * c, p);
       }
-      l += s0 + s1;
+      l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(&bars->p[i]);
@@ -399,7 +417,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       if (there && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -kInf : kLn2 * (m * F - kUp + log2f(l));
     }
     tc_fence_before();
-  } else if (work && warp < kSoftWarps + kDecWarps) {
+    }
+  } else if (warp < kSoftWarps + kDecWarps) {
+    registers_down<kDecRegs>();
+    if (work) {
     // ======================================================== decode
     // A lane takes 16 bytes of codes (32 dimensions) of a token; eight tokens side
     // by side fill a core matrix.
@@ -487,7 +508,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       fence_proxy_async_smem();
       mbar_arrive(&bars->vfull[st]);
     }
-  } else if (work && warp == kMmaWarp && lane == 0 && tiles > 0) {
+    }
+  } else {
+    registers_down<kMmaRegs>();
+    if (work && warp == kMmaWarp && lane == 0 && tiles > 0) {
     // ======================================================== MMA
     const uint32_t idS = idesc_f16_f32(kTile, kTile), idO = idesc_f16_f32(kTile, D) | (1u << 16);  // V: MN-major
     const uint32_t sQ = smem_u32(smem + Y::oQ), sK = smem_u32(smem + Y::oK), sV = smem_u32(smem + Y::oV);
@@ -531,6 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
           if (i == 1) mma_commit(&bars->kempty[nx]);
         }
       }
+    }
     }
   }
   __syncwarp();
