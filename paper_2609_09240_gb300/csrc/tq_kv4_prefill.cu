@@ -129,6 +129,38 @@ __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t b
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 __device__ __forceinline__ uint32_t as_bits(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
 
+// Four MMAs over successive steps of the contraction, in one piece: written one
+// by one, each waits for its descriptors' arithmetic (130 cycles between MMAs
+// that take 32).  acc: does the first add to what is there?
+template <int STEP_B>
+__device__ __forceinline__ void mma4_smemA(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n.reg .pred p, q;\n.reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      "setp.ne.b32 p, %4, 0;\nsetp.eq.b32 q, %3, %3;\n"
+      "add.s64 a1, %1, 16;\nadd.s64 a2, %1, 32;\nadd.s64 a3, %1, 48;\n"
+      "add.s64 b1, %2, %5;\nadd.s64 b2, %2, 2 * %5;\nadd.s64 b3, %2, 3 * %5;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, q;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, q;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, q;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc), "n"(STEP_B)
+      : "memory");
+}
+template <int STEP_B>
+__device__ __forceinline__ void mma4_tmemA(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n.reg .pred p, q;\n.reg .b32 a1, a2, a3;\n.reg .b64 b1, b2, b3;\n"
+      "setp.ne.b32 p, %4, 0;\nsetp.eq.b32 q, %3, %3;\n"
+      "add.s32 a1, %1, 8;\nadd.s32 a2, %1, 16;\nadd.s32 a3, %1, 24;\n"
+      "add.s64 b1, %2, %5;\nadd.s64 b2, %2, 2 * %5;\nadd.s64 b3, %2, 3 * %5;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, q;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, q;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, q;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(acc), "n"(STEP_B)
+      : "memory");
+}
+
 // The eight values of a code word, dimensions 0 4 1 5 2 6 3 7.
 __device__ __forceinline__ uint4 decode(uint32_t w, __half2 s, __half2 za, __half2 zb) {
   const uint32_t v = w >> 8;
@@ -515,18 +547,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
     // ======================================================== MMA
     const uint32_t idS = idesc_f16_f32(kTile, kTile), idO = idesc_f16_f32(kTile, D) | (1u << 16);  // V: MN-major
     const uint32_t sQ = smem_u32(smem + Y::oQ), sK = smem_u32(smem + Y::oK), sV = smem_u32(smem + Y::oV);
+    // a step is 16 dimensions (two core matrices of a row group) or 16 tokens (two row groups)
     auto scores = [&](int i, int st) {
-#pragma unroll 1
-      for (int k = 0; k < D / 16; ++k)
-        mma_smemA(tmem + i * kTile, smem_desc(sQ + i * Y::kTileBytes + k * 256, 128, C * 128),
-                  smem_desc(sK + st * Y::kTileBytes + k * 256, 128, C * 128), idS, k > 0);
+      const uint64_t q = smem_desc(sQ + i * Y::kTileBytes, 128, C * 128);
+      const uint64_t k = smem_desc(sK + st * Y::kTileBytes, 128, C * 128);
+#pragma unroll
+      for (int s4 = 0; s4 < D / 64; ++s4)
+        mma4_smemA<16>(tmem + i * kTile, q + s4 * 64, k + s4 * 64, idS, s4 > 0);
       mma_commit(&bars->s[i]);
     };
     auto values = [&](int i, int j) {
-#pragma unroll 1
-      for (int k = 0; k < kTile / 16; ++k)
-        mma_tmemA(tmem + 2 * kTile + i * D, tmem + i * kTile + k * 8,
-                  smem_desc(sV + (j & 1) * Y::kTileBytes + k * 2 * C * 128, C * 128, 128), idO, j > 0 || k > 0);
+      const uint64_t v = smem_desc(sV + (j & 1) * Y::kTileBytes, C * 128, 128);
+#pragma unroll
+      for (int s4 = 0; s4 < 2; ++s4)
+        mma4_tmemA<2 * C * 8>(tmem + 2 * kTile + i * D, tmem + i * kTile + s4 * 32, v + s4 * (4 * 2 * C * 8), idO,
+                              j > 0 || s4 > 0);
     };
     const int n0 = T.tiles[0], n1 = T.tiles[1];
     bool ok = wait(&bars->q, 0, abort_) && wait(&bars->kfull[0], 0, abort_);
