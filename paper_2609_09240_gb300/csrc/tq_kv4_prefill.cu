@@ -16,8 +16,8 @@
 // the keys 128 tokens (two pages) at a time:
 //   warps 0..3, 4..7   softmax of tile 0 and 1, a row per thread: S from tensor
 //                      memory, P back over it
-//   warps 8..15        decode K and V tiles (two stages each) for both tiles
-//   warp 16            one thread issues the MMAs: while one tile's softmax runs
+//   warps 8..11        decode K and V tiles (two stages each) for both tiles
+//   warp 12            one thread issues the MMAs: while one tile's softmax runs
 //                      the tensor cores work for the other
 // Tensor memory: S (P in its first half) of both tiles 2 x 128 columns, O 2 x D.
 // K tiles are K-major, V tiles the same bytes read MN-major (tokens are the
@@ -36,8 +36,8 @@ namespace kv4 {
 namespace pf {
 
 constexpr int kTile = 128;                   // tokens of a K/V tile, rows of a row tile
-constexpr int kSoftWarps = 8, kDecWarps = 8, kMmaWarp = 16;
-constexpr int kThreads = 20 * 32;  // five warpgroups, for their register counts
+constexpr int kSoftWarps = 8, kDecWarps = 4, kMmaWarp = 12;
+constexpr int kThreads = 16 * 32;  // four warpgroups, for their register counts
 constexpr int kDecThreads = kDecWarps * 32;
 constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr float kGrow = 8.0f, kUp = 7.0f;
@@ -99,15 +99,15 @@ __device__ __forceinline__ void tmem_wait32(uint32_t *r) {
                  "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
                  "+r"(r[30]), "+r"(r[31])::"memory");
 }
-// The warpgroup's registers per thread from here on.  640 threads are launched
-// with 96 each; what the warpgroups take is no more.
+// The warpgroup's registers per thread from here on.  512 threads are launched
+// with 128 each; what the warpgroups take is no more.
 #ifndef SR
-#define SR 160
-#define DR 56
-#define MR 48
+#define SR 168
+#define DR 112
+#define MR 64
 #endif
 constexpr int kSoftRegs = SR, kDecRegs = DR, kMmaRegs = MR;
-static_assert(256 * kSoftRegs + 256 * kDecRegs + 128 * kMmaRegs <= kThreads * 96, "registers of the launch");
+static_assert(256 * kSoftRegs + 128 * kDecRegs + 128 * kMmaRegs <= kThreads * 128, "registers of the launch");
 template <int N>
 __device__ __forceinline__ void registers_up() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -354,17 +354,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
         for (int k = 0; k < 32; ++k)
           if (32 * c + k < lo || 32 * c + k >= hi) x[k] = 0xFF800000u;
       };
-      uint32_t x[2][32];  // a piece at hand, the next one on its way
+      uint32_t x[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, x[c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_wait32(x[c]);
+      if (!plain)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) hide(c, x[c]);
       float top4[4] = {-kInf, -kInf, -kInf, -kInf};
-      tmem_ld32(tS, x[0]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        tmem_wait32(x[c & 1]);
-        tmem_ld32(tS + 32 * ((c + 1) & 3), x[(c + 1) & 1]);  // at last the first one again
-        if (!plain) hide(c, x[c & 1]);
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int k = 0; k < 32; ++k) top4[k & 3] = fmaxf(top4[k & 3], __uint_as_float(x[c & 1][k]));
-      }
+        for (int k = 0; k < 32; k += 2)
+          top4[k >> 1 & 3] = fmaxf(top4[k >> 1 & 3], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
       const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
       // rows whose maximum has grown by more than 2^8 take it as their reference
       const bool grow = top > m && (m == -kInf || (top - m) * F > kGrow);
@@ -395,18 +398,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
 #pragma unroll
             for (int gr = 0; gr < G; ++gr) lost |= (notes[4 * gr + (k >> 5)] >> (k & 31) & 1u) << gr;
       }
-      // P over the first half of S, in order: its piece c lies on what pieces 0 .. c / 2 were
       float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        tmem_wait32(x[c & 1]);
-        if (c < 3) tmem_ld32(tS + 32 * (c + 1), x[(c + 1) & 1]);
-        if (!plain) hide(c, x[c & 1]);
         uint32_t p[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-          const float p0 = exp2_fast(fmaf(__uint_as_float(x[c & 1][2 * k]), F, -ref));
-          const float p1 = exp2_fast(fmaf(__uint_as_float(x[c & 1][2 * k + 1]), F, -ref));
+          const float p0 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k]), F, -ref));
+          const float p1 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k + 1]), F, -ref));
           s4[2 * (k & 1)] += p0;
           s4[2 * (k & 1) + 1] += p1;
           p[k] = pack_out<false>(p0, p1);
