@@ -19,6 +19,17 @@ __device__ __forceinline__ float to_float(uint16_t b) {
   return BF16 ? __uint_as_float((uint32_t)b << 16) : __half2float(__ushort_as_half(b));
 }
 
+// rint(x / s) for |x / s| < 128, exactly as the definition has it (half to
+// even), with r = 1 / s: x has eleven significant bits and s seven, so a
+// quotient that is not half way between integers is at least 2^-14 from there,
+// and one that is comes out of x r within 2^-18 of it.  Rounding to multiples of
+// 2^-15 puts the second kind back on the half and leaves the first on its side.
+// (Dividing takes 26 us instead of 12 for 2000 tokens of a prompt.)
+__device__ __forceinline__ float nearest(float x, float r) {
+  const float q = __fadd_rn(__fadd_rn(__fmul_rn(x, r), 384.0f), -384.0f);
+  return __fadd_rn(__fadd_rn(q, 12582912.0f), -12582912.0f);
+}
+
 struct Rows {
   const uint16_t *k, *v;
   int64_t k_stride, v_stride;
@@ -72,7 +83,8 @@ __global__ void __launch_bounds__(kThreads)
       ((uint32_t)__half_as_ushort(__float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.0f))) + 15u) & 0xFFF0u;
   const float s = __half2float(__ushort_as_half((unsigned short)bits));
   const float div = s > 0.0f ? s : 1.0f;
-  const float z = fminf(fmaxf(rintf(__fdiv_rn(-lo, div)), 0.0f), 15.0f);
+  const float r = __frcp_rn(div);
+  const float z = fminf(fmaxf(nearest(-lo, r), 0.0f), 15.0f);
   uint32_t codes = 0;
   uint32_t param = bits | (uint32_t)z;
   if (!finite || bits >= 0x7C00u || s * fmaxf(z, 15.0f - z) > 65504.0f) {
@@ -80,7 +92,7 @@ __global__ void __launch_bounds__(kThreads)
   } else {
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      codes |= (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x[i], div)) + z, 0.0f), 15.0f) << (4 * i);
+      codes |= (uint32_t)fminf(fmaxf(nearest(x[i], r) + z, 0.0f), 15.0f) << (4 * i);
   }
   if (!there) return;
   const int w = where[t];

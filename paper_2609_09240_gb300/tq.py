@@ -769,30 +769,41 @@ _KV_DTYPE = {torch.float16: 0, torch.bfloat16: 1}
 
 
 def _want(t, name, dtype, shape=None):
-    """A contiguous CUDA tensor of the given type (and shape); its pointer."""
-    if t.dtype != dtype:
+    """The address of a contiguous CUDA tensor of the given type (and shape)."""
+    try:
+        if t.dtype is dtype and t.is_cuda and (shape is None or t.shape == shape) and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{name}: expected a torch tensor") from None
+    if t.dtype is not dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _p(t)
+    _p(t)
+    raise ValueError(f"{name}: expected a contiguous CUDA tensor")
 
 
 def _rows(t, name, heads, dim):
-    """(pointer, elements between tokens) of a [tokens][heads][dim] tensor whose
+    """(address, elements between tokens) of a [tokens][heads][dim] tensor whose
     heads lie side by side; tokens may be any distance apart."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("expected a torch tensor")
+    try:
+        shape, stride = t.shape, t.stride()
+    except AttributeError:
+        raise TypeError(f"{name}: expected a torch tensor") from None
     if not t.is_cuda:
         raise ValueError(f"{name}: expected a CUDA tensor (device memory)")
     if t.dtype not in _KV_DTYPE:
         raise ValueError(f"{name}: expected fp16 or bf16, got {t.dtype}")
-    T = t.shape[0]
-    if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name}: expected [tokens][{heads or 'heads'}][{dim}], got {tuple(t.shape)}")
-    if T and ((t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != dim)):
+    if len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name}: expected [tokens][{heads or 'heads'}][{dim}], got {tuple(shape)}")
+    if shape[0] and (stride[2] != 1 or (shape[1] > 1 and stride[1] != dim)):
         raise ValueError(f"{name}: the heads of a token must lie side by side")
-    row = t.shape[1] * dim
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if T > 1 else row)
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else shape[1] * dim)
+
+
+def _raw_stream(stream):
+    """The stream's handle as a number (the current stream's for None)."""
+    return _stream(stream).value or 0
 
 
 class Kv4Cache:
@@ -814,6 +825,7 @@ class Kv4Cache:
         c.data, c.table = _want(data, "data", torch.uint8), _want(table, "table", torch.int32)
         c.length, c.refs = (_want(length, "length", torch.int32, (slots,)), _want(refs, "refs", torch.int32, (pages,)))
         self._struct, self._ref = c, ctypes.byref(c)
+        self._status = self.status.data_ptr()
         self._ws, self._outgrown, self._sizes = {}, [], {}
 
     @classmethod
@@ -839,13 +851,13 @@ class Kv4Cache:
             if len(self._sizes) >= 4096:
                 self._sizes.clear()
             self._sizes[key] = n
-        ws = self._ws.get(stream.value)
+        ws = self._ws.get(stream)
         if ws is None or ws.numel() < n:
             if ws is not None:
                 self._outgrown.append(ws)
                 n = max(n, 2 * ws.numel())
-            ws = self._ws[stream.value] = workspace(n, self.data.device)
-        return ctypes.c_void_p(ws.data_ptr()), ws.numel()
+            ws = self._ws[stream] = workspace(n, self.data.device)
+        return ws.data_ptr(), ws.numel()
 
     def check(self):
         """Raise on data errors that earlier calls reported (synchronizes; clears them)."""
@@ -865,28 +877,28 @@ def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, wher
         indptr = torch.empty(n + 1, dtype=torch.int32, device=slots.device)
     if where is None:
         where = torch.empty(tokens, dtype=torch.int32, device=slots.device)
-    st = _stream(stream)
+    st = _raw_stream(stream)
     ws, nws = cache._scratch(st, "tq_kv4_extend_workspace_bytes", n, tokens)
     i32 = torch.int32
-    _check(lib().tq_kv4_extend(cache._ref, n, _want(slots, "slots", i32, (n,)), _want(counts, "counts", i32, (n,)),
+    _check((_lib or lib()).tq_kv4_extend(cache._ref, n, _want(slots, "slots", i32, (n,)), _want(counts, "counts", i32, (n,)),
                                tokens, _want(indptr, "indptr", i32, (n + 1,)), _want(where, "where", i32, (tokens,)), ws,
-                               nws, _p(cache.status), st), "tq_kv4_extend")
+                               nws, cache._status, st), "tq_kv4_extend")
     return indptr, where
 
 
 def tq_kv4_fork(cache: Kv4Cache, src, dst, stream=None):
     """Empty sequences dst[i] become copies of sequences src[i] that share their pages."""
     n = src.shape[0]
-    _check(lib().tq_kv4_fork(cache._ref, n, _want(src, "src", torch.int32, (n,)), _want(dst, "dst", torch.int32, (n,)),
-                             _p(cache.status), _stream(stream)), "tq_kv4_fork")
+    _check((_lib or lib()).tq_kv4_fork(cache._ref, n, _want(src, "src", torch.int32, (n,)), _want(dst, "dst", torch.int32, (n,)),
+                             cache._status, _raw_stream(stream)), "tq_kv4_fork")
 
 
 def tq_kv4_free(cache: Kv4Cache, slots, keep=None, stream=None):
     """Sequences slots[i] cut to keep[i] tokens (0 without keep)."""
     n = slots.shape[0]
     k = None if keep is None else _want(keep, "keep", torch.int32, (n,))
-    _check(lib().tq_kv4_free(cache._ref, n, _want(slots, "slots", torch.int32, (n,)), k, _p(cache.status),
-                             _stream(stream)), "tq_kv4_free")
+    _check((_lib or lib()).tq_kv4_free(cache._ref, n, _want(slots, "slots", torch.int32, (n,)), k, cache._status,
+                             _raw_stream(stream)), "tq_kv4_free")
 
 
 def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, live=None, stream=None):
@@ -898,12 +910,12 @@ def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, l
     refs_out = cache.refs if refs_out is None else refs_out
     remap = torch.empty(cache.pages, **i32) if remap is None else remap
     live = torch.empty(1, **i32) if live is None else live
-    st = _stream(stream)
+    st = _raw_stream(stream)
     ws, nws = cache._scratch(st, "tq_kv4_compact_workspace_bytes")
-    _check(lib().tq_kv4_compact(cache._ref, _want(table_out, "table_out", torch.int32, cache.table.shape),
+    _check((_lib or lib()).tq_kv4_compact(cache._ref, _want(table_out, "table_out", torch.int32, cache.table.shape),
                                 _want(refs_out, "refs_out", torch.int32, cache.refs.shape),
                                 _want(remap, "remap", torch.int32, (cache.pages,)),
-                                _want(live, "live", torch.int32, (1,)), ws, nws, _p(cache.status), st),
+                                _want(live, "live", torch.int32, (1,)), ws, nws, cache._status, st),
            "tq_kv4_compact")
     return remap, live
 
@@ -911,8 +923,8 @@ def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, l
 def tq_kv4_copy_pages(src: Kv4Cache, dst: Kv4Cache, src_pages, dst_pages, stream=None):
     """Page src_pages[i] of cache src, every layer, into page dst_pages[i] of cache dst."""
     n = src_pages.shape[0]
-    _check(lib().tq_kv4_copy_pages(src._ref, dst._ref, n, _want(src_pages, "src_pages", torch.int32, (n,)),
-                                   _want(dst_pages, "dst_pages", torch.int32, (n,)), _p(dst.status), _stream(stream)),
+    _check((_lib or lib()).tq_kv4_copy_pages(src._ref, dst._ref, n, _want(src_pages, "src_pages", torch.int32, (n,)),
+                                   _want(dst_pages, "dst_pages", torch.int32, (n,)), dst._status, _raw_stream(stream)),
            "tq_kv4_copy_pages")
 
 
@@ -924,8 +936,8 @@ def tq_kv4_append(k, v, cache: Kv4Cache, layer: int, where, stream=None):
     T = k.shape[0]
     if v.shape[0] != T or v.dtype != k.dtype:
         raise ValueError("k and v differ in tokens or type")
-    _check(lib().tq_kv4_append(cache._ref, layer, T, _KV_DTYPE[k.dtype], kp, ks, vp, vs,
-                               _want(where, "where", torch.int32, (T,)), _p(cache.status), _stream(stream)),
+    _check((_lib or lib()).tq_kv4_append(cache._ref, layer, T, _KV_DTYPE[k.dtype], kp, ks, vp, vs,
+                               _want(where, "where", torch.int32, (T,)), cache._status, _raw_stream(stream)),
            "tq_kv4_append")
 
 
@@ -937,9 +949,9 @@ def tq_kv4_read(cache: Kv4Cache, layer: int, where, dtype=torch.float16, k=None,
     v = torch.empty(shape, dtype=dtype, device=where.device) if v is None else v
     if dtype not in _KV_DTYPE:
         raise ValueError(f"expected fp16 or bf16, got {dtype}")
-    _check(lib().tq_kv4_read(cache._ref, layer, T, _KV_DTYPE[dtype], _want(where, "where", torch.int32, (T,)),
-                             _want(k, "k", dtype, shape), _want(v, "v", dtype, shape), _p(cache.status),
-                             _stream(stream)), "tq_kv4_read")
+    _check((_lib or lib()).tq_kv4_read(cache._ref, layer, T, _KV_DTYPE[dtype], _want(where, "where", torch.int32, (T,)),
+                             _want(k, "k", dtype, shape), _want(v, "v", dtype, shape), cache._status,
+                             _raw_stream(stream)), "tq_kv4_read")
     return k, v
 
 
@@ -959,13 +971,13 @@ def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, 
         raise ValueError("out and q differ in tokens or type")
     n = slots.shape[0]
     max_q = T if max_q is None else min(int(max_q), T)
-    st = _stream(stream)
+    st = _raw_stream(stream)
     ws, nws = cache._scratch(st, "tq_kv4_attention_workspace_bytes", n, T, max_q, Hq)
     lp = None if lse is None else _want(lse, "lse", torch.float32, (T, Hq))
-    _check(lib().tq_kv4_attention(cache._ref, layer, n, _want(slots, "slots", torch.int32, (n,)),
+    _check((_lib or lib()).tq_kv4_attention(cache._ref, layer, n, _want(slots, "slots", torch.int32, (n,)),
                                   _want(indptr, "indptr", torch.int32, (n + 1,)), T, max_q, Hq, _KV_DTYPE[q.dtype], qp,
                                   qs, cache.dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
-                                  int(window), op, os_, lp, ws, nws, _p(cache.status), st), "tq_kv4_attention")
+                                  int(window), op, os_, lp, ws, nws, cache._status, st), "tq_kv4_attention")
     return out
 
 
@@ -978,6 +990,8 @@ class W4Weight:
         s = tq_w4_weight(N, K)
         s.tiles = tiles.data_ptr()
         self._struct, self._ref = s, ctypes.byref(s)
+        # the product needs no scratch memory; the argument has to be there
+        self._ws = workspace(256, tiles.device)
 
     @classmethod
     def _new(cls, N, K, device):
@@ -1007,7 +1021,7 @@ def pack_w4(codes, scale, minimum, stream=None, check=True) -> W4Weight:
     g = (N, K // TQ_GROUP)
     cp, sp, mp = (_want(codes, "codes", torch.uint8), _want(scale, "scale", torch.float16, g),
                   _want(minimum, "minimum", torch.float16, g))
-    _w4_made(lambda st: lib().tq_w4_pack(N, K, cp, sp, mp, _p(w.tiles), st, _stream(stream)), "tq_w4_pack",
+    _w4_made(lambda st: lib().tq_w4_pack(N, K, cp, sp, mp, _p(w.tiles), st, _raw_stream(stream)), "tq_w4_pack",
              codes.device, check)
     return w
 
@@ -1017,7 +1031,7 @@ def quantize_w4(W, stream=None, check=True) -> W4Weight:
     N, K = W.shape
     w = W4Weight._new(N, K, W.device)
     wp = _want(W, "W", torch.float16)
-    _w4_made(lambda st: lib().tq_w4_quantize(N, K, wp, _p(w.tiles), st, _stream(stream)), "tq_w4_quantize", W.device,
+    _w4_made(lambda st: lib().tq_w4_quantize(N, K, wp, _p(w.tiles), st, _raw_stream(stream)), "tq_w4_quantize", W.device,
              check)
     return w
 
@@ -1026,7 +1040,7 @@ def tq_w4_dequantize(w: W4Weight, out=None, stream=None):
     """W as dense fp16 [N][K] on the device."""
     if out is None:
         out = torch.empty((w.N, w.K), dtype=torch.float16, device=w.tiles.device)
-    _check(lib().tq_w4_dequantize(w.N, w.K, w._ref, _want(out, "out", torch.float16, (w.N, w.K)), _stream(stream)),
+    _check((_lib or lib()).tq_w4_dequantize(w.N, w.K, w._ref, _want(out, "out", torch.float16, (w.N, w.K)), _raw_stream(stream)),
            "tq_w4_dequantize")
     return out
 
@@ -1039,10 +1053,9 @@ def tq_w4_linear(x, w: W4Weight, y=None, ws=None, stream=None, f32=False):
     if y is None:
         y = torch.empty((M, w.N), dtype=dt, device=x.device)
     if ws is None:
-        n = int(lib().tq_w4_workspace_bytes(M, w.N, w.K))
-        if n == 0:
-            raise TQError(-2, "tq_w4_workspace_bytes")
-        ws = workspace(n, x.device)
-    fn = lib().tq_w4_linear_f32out if f32 else lib().tq_w4_linear
-    _check(fn(M, w.N, w.K, w._ref, xp, _want(y, "y", dt, (M, w.N)), _p(ws), ws.numel(), _stream(stream)), "tq_w4_linear")
+        ws = w._ws
+    L = _lib or lib()
+    fn = L.tq_w4_linear_f32out if f32 else L.tq_w4_linear
+    _check(fn(M, w.N, w.K, w._ref, xp, _want(y, "y", dt, (M, w.N)), _want(ws, "ws", torch.uint8), ws.numel(),
+              _raw_stream(stream)), "tq_w4_linear")
     return y
