@@ -38,16 +38,13 @@ struct Rows {
 // One item = (token, K or V, head), D / 8 threads.
 template <int D, bool BF16, bool VEC>
 __global__ void __launch_bounds__(kThreads)
-    append_kernel(const tq_kv4_cache c, int layer, int64_t items, Rows in, const int32_t *__restrict__ where,
+    append_kernel(const tq_kv4_cache c, int layer, uint32_t items, Rows in, const int32_t *__restrict__ where,
                   uint32_t *d_status) {
   using B = Block<D>;
   constexpr int TPI = D / kPer;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t item = idx / TPI;
-  const int part = (int)(idx % TPI);
+  const uint32_t item = blockIdx.x * (kThreads / TPI) + threadIdx.x / TPI, part = threadIdx.x % TPI;
   const bool there = item < items;
-  const int h = there ? (int)(item % c.heads) : 0;
-  const int64_t th = there ? item / c.heads : 0;
+  const uint32_t th = there ? item / (uint32_t)c.heads : 0, h = there ? item - th * c.heads : 0;
   const bool val = th & 1;
   const int64_t t = th >> 1;
   const uint16_t *src = (val ? in.v + t * in.v_stride : in.k + t * in.k_stride) + h * D + part * kPer;
@@ -92,7 +89,8 @@ __global__ void __launch_bounds__(kThreads)
   } else {
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      codes |= (uint32_t)fminf(fmaxf(nearest(x[i], r) + z, 0.0f), 15.0f) << (4 * i);
+      // the integer from the low bits of 2^23 + c: a conversion would take a slower pipe
+      codes |= (__float_as_uint(__fadd_rn(fminf(fmaxf(nearest(x[i], r) + z, 0.0f), 15.0f), 8388608.0f)) & 15u) << (4 * i);
   }
   if (!there) return;
   const int w = where[t];
@@ -111,16 +109,13 @@ __global__ void __launch_bounds__(kThreads)
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads)
-    read_kernel(const tq_kv4_cache c, int layer, int64_t items, const int32_t *__restrict__ where, uint16_t *k,
+    read_kernel(const tq_kv4_cache c, int layer, uint32_t items, const int32_t *__restrict__ where, uint16_t *k,
                 uint16_t *v, uint32_t *d_status) {
   using B = Block<D>;
   constexpr int TPI = D / kPer;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t item = idx / TPI;
-  const int part = (int)(idx % TPI);
+  const uint32_t item = blockIdx.x * (kThreads / TPI) + threadIdx.x / TPI, part = threadIdx.x % TPI;
   if (item >= items) return;
-  const int h = (int)(item % c.heads);
-  const int64_t th = item / c.heads;
+  const uint32_t th = item / (uint32_t)c.heads, h = item - th * c.heads;
   const bool val = th & 1;
   const int64_t t = th >> 1;
   grid_dep_wait();
@@ -132,13 +127,25 @@ __global__ void __launch_bounds__(kThreads)
     const uint32_t codes = *reinterpret_cast<const uint32_t *>(blk + (val ? B::oV : B::oK) + off * B::kRow + part * 4);
     const uint32_t p = *reinterpret_cast<const uint16_t *>(blk + (val ? B::oPV : B::oPK) +
                                                            (part / (kGrp / kPer) * kPage + off) * 2);
-    const float s = param_scale(p), z = param_zero(p);
+    // (1024 + c) - (1024 + z), times s: exact in fp16 (nibbles i and 4 + i together)
+    const uint32_t z = (p & 15u) * 0x10001u, sc = (p & 0xFFF0u) * 0x10001u;
+    uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const float x = s * ((float)((codes >> (4 * i)) & 15u) - z);  // exact
-      const uint32_t b = BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x))
-                              : (uint32_t)__half_as_ushort(__float2half_rn(x));
-      out[i >> 1] |= b << (16 * (i & 1));
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t c = (codes >> (4 * i) & 0x000F000Fu) | 0x64006400u, za = z | 0x64006400u;
+      const __half2 d = __hmul2(__hsub2(*reinterpret_cast<const __half2 *>(&c), *reinterpret_cast<const __half2 *>(&za)),
+                                *reinterpret_cast<const __half2 *>(&sc));
+      v[i] = *reinterpret_cast<const uint32_t *>(&d);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t h = __byte_perm(v[2 * (i & 1)], v[2 * (i & 1) + 1], i < 2 ? 0x5410 : 0x7632);
+      if (BF16) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out[i]) : "f"(f.y), "f"(f.x));
+      } else {
+        out[i] = h;
+      }
     }
   } else if (w >= 0 && part == 0) {
     report(d_status, TQ_DATA_BAD_SLOT);
@@ -147,10 +154,11 @@ __global__ void __launch_bounds__(kThreads)
   *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
+// Items are counted in 32 bits (a 64-bit division per thread was half of the
+// instructions).
 inline bool grid_of(int64_t items, int D, unsigned *grid) {
-  const int64_t n = (items * (D / kPer) + kThreads - 1) / kThreads;
-  *grid = (unsigned)n;
-  return n <= 0x7fffffff;
+  *grid = (unsigned)((items * (D / kPer) + kThreads - 1) / kThreads);
+  return items <= 0x7fffffff;
 }
 
 }  // namespace kv4
@@ -180,7 +188,7 @@ tq_status tq_kv4_append(const tq_kv4_cache *c, int32_t layer, int32_t tokens, in
   const bool vec = aligned_to(k, 16) && aligned_to(v, 16) && k_stride % 8 == 0 && v_stride % 8 == 0;
   const Rows in = {k, v, k_stride, v_stride};
   auto go = [&](auto kern) {
-    return from_cuda(launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, items, in, where,
+    return from_cuda(launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, (uint32_t)items, in, where,
                                       d_status));
   };
   const bool bf = dtype == TQ_BF16;
@@ -205,7 +213,7 @@ tq_status tq_kv4_read(const tq_kv4_cache *c, int32_t layer, int32_t tokens, int3
   if (!grid_of(items, c->dim, &grid)) return TQ_ERR_SHAPE;
   auto go = [&](auto kern) {
     return from_cuda(
-        launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, items, where, k, v, d_status));
+        launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, (uint32_t)items, where, k, v, d_status));
   };
   if (c->dim == 128) return dtype == TQ_BF16 ? go(read_kernel<128, true>) : go(read_kernel<128, false>);
   return dtype == TQ_BF16 ? go(read_kernel<64, true>) : go(read_kernel<64, false>);
