@@ -824,10 +824,20 @@ inline size_t split_ws_bytes(int D, int NT) {
   const int warps = NT == 1 ? Shape<128, 1>::kWarps : Shape<128, 2>::kWarps;
   return (size_t)sm_count() * warps * (sizeof(Join) + 2 * (8 * NT) * (D + 2) * 4);
 }
-#ifndef MANY
-#define MANY 64
-#endif
-constexpr int kManyRows = MANY;
+// Which kernel a sequence's rows go to.  The kernel for many rows takes 256 of
+// them at a time, 2.3 us per 128 keys whatever their number, and a block does a
+// task to its end; the kernel for few rows spreads a chip-wide 2.9 ns per 64 keys,
+// head and 16 rows evenly.  They meet at 6000 rows (of all heads and sequences)
+// per wave of blocks: for 16 sequences with 8 K/V heads 48 rows each take 65 us in
+// the one and 58 in the other, 32 rows 48 and 57; for one sequence with 8 heads of
+// 6000 keys 256 rows take 49 and 106.  Within a call, sequences with fewer than 48
+// rows per head (a decode step among prompts) stay with the kernel for few.
+constexpr int kManyRows = 48, kManyAtOnce = 6000;
+inline bool many_rows(int64_t tokens, int max_q, int q_heads, int heads) {
+  const int64_t rows = tokens * q_heads, sms = sm_count();
+  const int64_t waves = std::max<int64_t>(1, (rows + 256 * sms - 1) / (256 * sms));
+  return (int64_t)max_q * (q_heads / heads) >= kManyRows && rows >= kManyAtOnce * waves;
+}
 inline int split_tiles(int max_q, int group) { return (int64_t)max_q * group <= 8 ? 1 : 2; }
 
 template <int D, int NT, bool BF16>
@@ -894,9 +904,10 @@ tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t count, 
   if (workspace_bytes < tq_kv4_attention_workspace_bytes(c, count, tokens, max_q, q_heads)) return TQ_ERR_SHAPE;
   if (tokens == 0) return TQ_OK;
   const int g = q_heads / c->heads;
-  const bool many = (int64_t)max_q * g >= kManyRows, bf16 = dtype == TQ_BF16;
-  const AttnArgs a = {*c,  layer,    count,      tokens, q_heads, causal != 0,                     window, slots, indptr, q, out, lse,
-                      q_stride, out_stride, scale,  d_status, many ? kManyRows : 0x7fffffff};
+  const bool many = many_rows(tokens, max_q, q_heads, c->heads), bf16 = dtype == TQ_BF16;
+  const AttnArgs a = {*c,  layer,    count,      tokens, q_heads,  causal != 0, window,
+                      slots, indptr, q,          out,    lse,      q_stride,    out_stride,
+                      scale, d_status, many ? kManyRows : 0x7fffffff};
   cudaStream_t st = (cudaStream_t)stream;
   if (many) {
     const cudaError_t e = launch_attn_prefill(a, bf16, st);

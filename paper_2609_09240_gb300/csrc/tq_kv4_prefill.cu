@@ -101,12 +101,7 @@ __device__ __forceinline__ void tmem_wait32(uint32_t *r) {
 }
 // The warpgroup's registers per thread from here on.  512 threads are launched
 // with 128 each; what the warpgroups take is no more.
-#ifndef SR
-#define SR 168
-#define DR 112
-#define MR 64
-#endif
-constexpr int kSoftRegs = SR, kDecRegs = DR, kMmaRegs = MR;
+constexpr int kSoftRegs = 168, kDecRegs = 112, kMmaRegs = 64;
 static_assert(256 * kSoftRegs + 128 * kDecRegs + 128 * kMmaRegs <= kThreads * 128, "registers of the launch");
 template <int N>
 __device__ __forceinline__ void registers_up() {
@@ -306,329 +301,329 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
   if (warp < kSoftWarps) {
     registers_up<kSoftRegs>();
     if (work) {
-    // ======================================================== softmax, a row per thread
-    const int i = warp >> 2, r = tid & 127;  // row tile and row
-    const int row = T.row0 + i * kTile + r;
-    const bool there = i * kTile + r < T.rows;
-    const int64_t token = T.q0 + (there ? row / g : 0);
-    const int head = T.h * g + (there ? row % g : 0);
-    // ---- Q: fp16, in the decoding's order of dimensions
-    float F = 1.0f;
-    {
-      const uint4 *src = reinterpret_cast<const uint4 *>(a.q + token * a.q_stride + head * D);
-      unsigned char *dst = smem + Y::oQ + i * Y::kTileBytes + ((r >> 3) * C) * 128 + (r & 7) * 16;
-      float up = 1.0f;
-      int e = 0;
-      if (BF16) {  // a power of two brings the row's largest value into [2^10, 2^11)
-        float top = 0.0f;
-        if (there)
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const uint4 v = __ldg(src + c);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xFFFF0000u))));
-          }
-        if (top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
-        up = __uint_as_float((uint32_t)(127 + e) << 23);
-      }
-      // a negative scale turns the queries' sign, none makes them zeros: F > 0
-      up = a.scale < 0.0f ? -up : a.scale == 0.0f ? 0.0f : up;
-      if (a.scale != 0.0f) F = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-37f);
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const uint4 v = there ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        float f[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          f[2 * k] = BF16 ? __uint_as_float(w[k] << 16) : __half2float(__ushort_as_half((uint16_t)w[k]));
-          f[2 * k + 1] =
-              BF16 ? __uint_as_float(w[k] & 0xFFFF0000u) : __half2float(__ushort_as_half((uint16_t)(w[k] >> 16)));
-        }
-        uint32_t o[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = pack_out<false>(f[k] * up, f[4 + k] * up);
-        *reinterpret_cast<uint4 *>(dst + c * 128) = make_uint4(o[0], o[1], o[2], o[3]);
-      }
-    }
-    fence_proxy_async_smem();
-    mbar_arrive(&bars->q);
-    // ---- what the row sees: [begin, end)
-    const int pos = T.L - T.n + row / g;
-    const int end = !there ? 0 : a.causal ? pos + 1 : T.L, begin = a.window > 0 ? pos - a.window + 1 : 0;
-    // what every row of the tile sees
-    const int pos_lo = T.L - T.n + (T.row0 + i * kTile) / g;
-    const int pos_hi = T.L - T.n + (T.row0 + min(T.rows, (i + 1) * kTile) - 1) / g;
-    const int all_end = a.causal ? pos_lo + 1 : T.L, all_begin = a.window > 0 ? pos_hi - a.window + 1 : 0;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 (warp % 4) in the lane field
-    const uint32_t tS = tmem + i * kTile + lanes, tO = tmem + 2 * kTile + i * D + lanes;
-    float m = -kInf, l = 0.0f;  // the reference of the exponentials (a score before F) and the sum
-    uint32_t lost = 0;          // groups with a NaN that the row sees
-    const int n = T.tiles[i];
-    bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      if (!__all_sync(0xffffffffu, wait(&bars->s[i], j & 1, abort_))) {
-        ok = false;
-        break;
-      }
-      tc_fence_after();
-      const int tok = T.t0 + j * kTile;
-      const bool plain = tok >= all_begin && tok + kTile <= all_end;
-      // the columns that the row sees
-      const int lo = max(begin - tok, 0), hi = min(end - tok, kTile);
-      // columns 32 c .. 32 c + 31: what is not seen at -inf
-      auto hide = [&](int c, uint32_t *x) {
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-          if (32 * c + k < lo || 32 * c + k >= hi) x[k] = 0xFF800000u;
-      };
-      uint32_t x[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, x[c]);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_wait32(x[c]);
-      if (!plain)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) hide(c, x[c]);
-      float top4[4] = {-kInf, -kInf, -kInf, -kInf};
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int k = 0; k < 32; k += 2)
-          top4[k >> 1 & 3] = fmaxf(top4[k >> 1 & 3], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
-      const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
-      // rows whose maximum has grown by more than 2^8 take it as their reference
-      const bool grow = top > m && (m == -kInf || (top - m) * F > kGrow);
-      if (__any_sync(0xffffffffu, grow && m != -kInf)) {
-        const float f = grow && m != -kInf ? exp2_fast((m - top) * F) : 1.0f;
-        l *= f;
-#pragma unroll 1
-        for (int c = 0; c < D / 16; ++c) {
-          uint32_t o[16];
-          tmem_ld_cols<16>(tO + 16 * c, o);
-          tmem_wait_ld();
-#pragma unroll
-          for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-          tmem_st16(tO + 16 * c, o);
-        }
-      }
-      if (grow) m = top;
-      const float ref = m == -kInf ? 0.0f : m * F - kUp;
-      // tokens that stand for NaN in V were decoded as zeros
+      // ======================================================== softmax, a row per thread
+      const int i = warp >> 2, r = tid & 127;  // row tile and row
+      const int row = T.row0 + i * kTile + r;
+      const bool there = i * kTile + r < T.rows;
+      const int64_t token = T.q0 + (there ? row / g : 0);
+      const int head = T.h * g + (there ? row % g : 0);
+      // ---- Q: fp16, in the decoding's order of dimensions
+      float F = 1.0f;
       {
-        const uint32_t *notes = reinterpret_cast<const uint32_t *>(smem + Y::oLost + (j & 3) * G * 16);
-        uint32_t any = 0;
+        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + token * a.q_stride + head * D);
+        unsigned char *dst = smem + Y::oQ + i * Y::kTileBytes + ((r >> 3) * C) * 128 + (r & 7) * 16;
+        float up = 1.0f;
+        int e = 0;
+        if (BF16) {  // a power of two brings the row's largest value into [2^10, 2^11)
+          float top = 0.0f;
+          if (there)
 #pragma unroll
-        for (int k = 0; k < 4 * G; ++k) any |= notes[k];
-        if (any)
-#pragma unroll 1
-          for (int k = lo; k < hi; ++k)
+            for (int c = 0; c < C; ++c) {
+              const uint4 v = __ldg(src + c);
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) lost |= (notes[4 * gr + (k >> 5)] >> (k & 31) & 1u) << gr;
-      }
-      float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t p[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float p0 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k]), F, -ref));
-          const float p1 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k + 1]), F, -ref));
-          s4[2 * (k & 1)] += p0;
-          s4[2 * (k & 1) + 1] += p1;
-          p[k] = pack_out<false>(p0, p1);
+              for (int k = 0; k < 4; ++k)
+                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xFFFF0000u))));
+            }
+          if (top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
+          up = __uint_as_float((uint32_t)(127 + e) << 23);
         }
-        tmem_st16(tS + 16 * c, p);
-      }
-      l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->p[i]);
-    }
-    // ---- the result
-    if (n > 0 && ok) ok = __all_sync(0xffffffffu, wait(&bars->o[i], 0, abort_));
-    if (ok) {
-      tc_fence_after();
-      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      uint16_t *out = a.out + token * a.out_stride + head * D;
+        // a negative scale turns the queries' sign, none makes them zeros: F > 0
+        up = a.scale < 0.0f ? -up : a.scale == 0.0f ? 0.0f : up;
+        if (a.scale != 0.0f) F = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-37f);
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        float x[32];
+        for (int c = 0; c < C; ++c) {
+          const uint4 v = there ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          float f[8];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = 0.0f;
-        if (n > 0) {
-          tmem_ld32(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
-          tmem_wait_ld();
-        }
-        const bool nan = lost >> (32 * c / kGrp) & 1;
-        if (there)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float f[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              f[k] = nan ? kInf - kInf : l == 0.0f ? 0.0f : x[8 * q + (k < 4 ? 2 * k : 2 * k - 7)] * inv;
-            *reinterpret_cast<uint4 *>(out + 32 * c + 8 * q) =
-                make_uint4(pack_out<BF16>(f[0], f[1]), pack_out<BF16>(f[2], f[3]), pack_out<BF16>(f[4], f[5]),
-                           pack_out<BF16>(f[6], f[7]));
+          for (int k = 0; k < 4; ++k) {
+            f[2 * k] = BF16 ? __uint_as_float(w[k] << 16) : __half2float(__ushort_as_half((uint16_t)w[k]));
+            f[2 * k + 1] =
+                BF16 ? __uint_as_float(w[k] & 0xFFFF0000u) : __half2float(__ushort_as_half((uint16_t)(w[k] >> 16)));
           }
+          uint32_t o[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = pack_out<false>(f[k] * up, f[4 + k] * up);
+          *reinterpret_cast<uint4 *>(dst + c * 128) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
       }
-      if (there && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -kInf : kLn2 * (m * F - kUp + log2f(l));
-    }
-    tc_fence_before();
+      fence_proxy_async_smem();
+      mbar_arrive(&bars->q);
+      // ---- what the row sees: [begin, end)
+      const int pos = T.L - T.n + row / g;
+      const int end = !there ? 0 : a.causal ? pos + 1 : T.L, begin = a.window > 0 ? pos - a.window + 1 : 0;
+      // what every row of the tile sees
+      const int pos_lo = T.L - T.n + (T.row0 + i * kTile) / g;
+      const int pos_hi = T.L - T.n + (T.row0 + min(T.rows, (i + 1) * kTile) - 1) / g;
+      const int all_end = a.causal ? pos_lo + 1 : T.L, all_begin = a.window > 0 ? pos_hi - a.window + 1 : 0;
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 (warp % 4) in the lane field
+      const uint32_t tS = tmem + i * kTile + lanes, tO = tmem + 2 * kTile + i * D + lanes;
+      float m = -kInf, l = 0.0f;  // the reference of the exponentials (a score before F) and the sum
+      uint32_t lost = 0;          // groups with a NaN that the row sees
+      const int n = T.tiles[i];
+      bool ok = true;
+      for (int j = 0; j < n; ++j) {
+        if (!__all_sync(0xffffffffu, wait(&bars->s[i], j & 1, abort_))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const int tok = T.t0 + j * kTile;
+        const bool plain = tok >= all_begin && tok + kTile <= all_end;
+        // the columns that the row sees
+        const int lo = max(begin - tok, 0), hi = min(end - tok, kTile);
+        // columns 32 c .. 32 c + 31: what is not seen at -inf
+        auto hide = [&](int c, uint32_t *x) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (32 * c + k < lo || 32 * c + k >= hi) x[k] = 0xFF800000u;
+        };
+        uint32_t x[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, x[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_wait32(x[c]);
+        if (!plain)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) hide(c, x[c]);
+        float top4[4] = {-kInf, -kInf, -kInf, -kInf};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int k = 0; k < 32; k += 2)
+            top4[k >> 1 & 3] = fmaxf(top4[k >> 1 & 3], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
+        const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+        // rows whose maximum has grown by more than 2^8 take it as their reference
+        const bool grow = top > m && (m == -kInf || (top - m) * F > kGrow);
+        if (__any_sync(0xffffffffu, grow && m != -kInf)) {
+          const float f = grow && m != -kInf ? exp2_fast((m - top) * F) : 1.0f;
+          l *= f;
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t o[16];
+            tmem_ld_cols<16>(tO + 16 * c, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st16(tO + 16 * c, o);
+          }
+        }
+        if (grow) m = top;
+        const float ref = m == -kInf ? 0.0f : m * F - kUp;
+        // tokens that stand for NaN in V were decoded as zeros
+        {
+          const uint32_t *notes = reinterpret_cast<const uint32_t *>(smem + Y::oLost + (j & 3) * G * 16);
+          uint32_t any = 0;
+#pragma unroll
+          for (int k = 0; k < 4 * G; ++k) any |= notes[k];
+          if (any)
+#pragma unroll 1
+            for (int k = lo; k < hi; ++k)
+#pragma unroll
+              for (int gr = 0; gr < G; ++gr) lost |= (notes[4 * gr + (k >> 5)] >> (k & 31) & 1u) << gr;
+        }
+        float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t p[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float p0 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k]), F, -ref));
+            const float p1 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k + 1]), F, -ref));
+            s4[2 * (k & 1)] += p0;
+            s4[2 * (k & 1) + 1] += p1;
+            p[k] = pack_out<false>(p0, p1);
+          }
+          tmem_st16(tS + 16 * c, p);
+        }
+        l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->p[i]);
+      }
+      // ---- the result
+      if (n > 0 && ok) ok = __all_sync(0xffffffffu, wait(&bars->o[i], 0, abort_));
+      if (ok) {
+        tc_fence_after();
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *out = a.out + token * a.out_stride + head * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          float x[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = 0.0f;
+          if (n > 0) {
+            tmem_ld32(tO + 32 * c, reinterpret_cast<uint32_t *>(x));
+            tmem_wait_ld();
+          }
+          const bool nan = lost >> (32 * c / kGrp) & 1;
+          if (there)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float f[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                f[k] = nan ? kInf - kInf : l == 0.0f ? 0.0f : x[8 * q + (k < 4 ? 2 * k : 2 * k - 7)] * inv;
+              *reinterpret_cast<uint4 *>(out + 32 * c + 8 * q) =
+                  make_uint4(pack_out<BF16>(f[0], f[1]), pack_out<BF16>(f[2], f[3]), pack_out<BF16>(f[4], f[5]),
+                             pack_out<BF16>(f[6], f[7]));
+            }
+        }
+        if (there && a.lse) a.lse[token * a.q_heads + head] = l == 0.0f ? -kInf : kLn2 * (m * F - kUp + log2f(l));
+      }
+      tc_fence_before();
     }
   } else if (warp < kSoftWarps + kDecWarps) {
     registers_down<kDecRegs>();
     if (work) {
-    // ======================================================== decode
-    // A lane takes 16 bytes of codes (32 dimensions) of a token; eight tokens side
-    // by side fill a core matrix.
-    constexpr int Q = D / 32, ITEMS = kTile * Q / kDecThreads, OPW = 4 / Q;  // octets that a warp covers at once
-    const int dw = warp - kSoftWarps, q = (lane >> 3) % Q;
-    int octet[ITEMS];
+      // ======================================================== decode
+      // A lane takes 16 bytes of codes (32 dimensions) of a token; eight tokens side
+      // by side fill a core matrix.
+      constexpr int Q = D / 32, ITEMS = kTile * Q / kDecThreads, OPW = 4 / Q;  // octets that a warp covers at once
+      const int dw = warp - kSoftWarps, q = (lane >> 3) % Q;
+      int octet[ITEMS];
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) octet[k] = (dw + k * kDecWarps) * OPW + (lane >> 3) / Q;
-    const int gr = q * 32 / kGrp;
-    const int32_t *table = a.c.table + (int64_t)T.slot * a.c.max_pages;
-    const int pages = (T.L + kPage - 1) / kPage;
-    struct Raw {
-      uint4 k, v;
-      uint32_t pk, pv;
-    } raw[ITEMS];
-    // a tile's two table entries are read two tiles ahead and looked at one later
-    int entry[2];
-    auto look_up = [&](int j) {
+      for (int k = 0; k < ITEMS; ++k) octet[k] = (dw + k * kDecWarps) * OPW + (lane >> 3) / Q;
+      const int gr = q * 32 / kGrp;
+      const int32_t *table = a.c.table + (int64_t)T.slot * a.c.max_pages;
+      const int pages = (T.L + kPage - 1) / kPage;
+      struct Raw {
+        uint4 k, v;
+        uint32_t pk, pv;
+      } raw[ITEMS];
+      // a tile's two table entries are read two tiles ahead and looked at one later
+      int entry[2];
+      auto look_up = [&](int j) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int pg = T.t0 / kPage + 2 * j + h;
-        entry[h] = pg < pages ? __ldg(table + pg) : -1;
-      }
-    };
-    auto load = [&](int j) {
-      const uint8_t *blk[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int p = entry[h];
-        const bool there = p >= 0 && p < a.c.pages;
-        if (!there && T.t0 / kPage + 2 * j + h < pages) report(a.d_status, TQ_DATA_BAD_SLOT);
-        blk[h] = there ? a.c.data + (((int64_t)a.layer * a.c.pages + p) * a.c.heads + T.h) * B::kBytes : nullptr;
-      }
-#pragma unroll
-      for (int k = 0; k < ITEMS; ++k) {
-        Raw &w = raw[k];
-        w.k = w.v = make_uint4(0, 0, 0, 0);
-        w.pk = w.pv = 0;
-        const int at = octet[k] * 8 + (lane & 7), off = at & (kPage - 1);
-        const uint8_t *p = blk[k >= ITEMS / 2];
-        if (p && T.t0 + j * kTile + at < T.L) {
-          w.k = __ldg(reinterpret_cast<const uint4 *>(p + B::oK + off * B::kRow + q * 16));
-          w.v = __ldg(reinterpret_cast<const uint4 *>(p + B::oV + off * B::kRow + q * 16));
-          w.pk = __ldg(reinterpret_cast<const uint16_t *>(p + B::oPK + (gr * kPage + off) * 2));
-          w.pv = __ldg(reinterpret_cast<const uint16_t *>(p + B::oPV + (gr * kPage + off) * 2));
+        for (int h = 0; h < 2; ++h) {
+          const int pg = T.t0 / kPage + 2 * j + h;
+          entry[h] = pg < pages ? __ldg(table + pg) : -1;
         }
-      }
-    };
-    static_assert(kTile == 2 * kPage && ITEMS % 2 == 0, "the first half of the items lies in a tile's first page");
-    look_up(0);
-    load(0);
-    look_up(1);
-    auto put = [&](unsigned char *tile, int k, const uint4 &codes, uint32_t param) {
-      const uint32_t z = (param & 15u) * 0x10001u;
-      const __half2 za = as_half2(z | 0x64006400u), zb = as_half2(z << 4 | 0x54005400u);
-      const __half2 s = as_half2((param & 0xFFF0u) * 0x10001u);
-      unsigned char *dst = tile + (octet[k] * C + 4 * q) * 128 + (lane & 7) * 16;
-      *reinterpret_cast<uint4 *>(dst) = decode(codes.x, s, za, zb);
-      *reinterpret_cast<uint4 *>(dst + 128) = decode(codes.y, s, za, zb);
-      *reinterpret_cast<uint4 *>(dst + 256) = decode(codes.z, s, za, zb);
-      *reinterpret_cast<uint4 *>(dst + 384) = decode(codes.w, s, za, zb);
-    };
-    for (int j = 0; j < tiles; ++j) {
-      const int st = j & 1;
-      Raw cur[ITEMS];
+      };
+      auto load = [&](int j) {
+        const uint8_t *blk[2];
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k) cur[k] = raw[k];
-      if (j + 1 < tiles) {
-        load(j + 1);
-        look_up(j + 2);
-      }
-      if (j >= 2 && !__all_sync(0xffffffffu, wait(&bars->kempty[st], ((j >> 1) & 1) ^ 1, abort_))) break;
+        for (int h = 0; h < 2; ++h) {
+          const int p = entry[h];
+          const bool there = p >= 0 && p < a.c.pages;
+          if (!there && T.t0 / kPage + 2 * j + h < pages) report(a.d_status, TQ_DATA_BAD_SLOT);
+          blk[h] = there ? a.c.data + (((int64_t)a.layer * a.c.pages + p) * a.c.heads + T.h) * B::kBytes : nullptr;
+        }
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k) {
-        put(smem + Y::oK + st * Y::kTileBytes, k, cur[k].k, cur[k].pk);
-        // Values that stand for NaN become zeros (0 times NaN must not count) and are noted for
-        // the rows that see them, with the tile's scores.  Four tiles' notes: the values of the
-        // tile before this one went to a stage whose tile, three before, every row was done with.
-        const uint32_t bits = __ballot_sync(0xffffffffu, (cur[k].pv & 0x7C00u) == 0x7C00u);
-        if ((lane & 7) == 0 && q * 32 % kGrp == 0)
-          smem[Y::oLost + ((j & 3) * G + gr) * 16 + octet[k]] = (unsigned char)(bits >> lane);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->kfull[st]);
-      if (j >= 2 && !__all_sync(0xffffffffu, wait(&bars->vempty[st], ((j >> 1) & 1) ^ 1, abort_))) break;
+        for (int k = 0; k < ITEMS; ++k) {
+          Raw &w = raw[k];
+          w.k = w.v = make_uint4(0, 0, 0, 0);
+          w.pk = w.pv = 0;
+          const int at = octet[k] * 8 + (lane & 7), off = at & (kPage - 1);
+          const uint8_t *p = blk[k >= ITEMS / 2];
+          if (p && T.t0 + j * kTile + at < T.L) {
+            w.k = __ldg(reinterpret_cast<const uint4 *>(p + B::oK + off * B::kRow + q * 16));
+            w.v = __ldg(reinterpret_cast<const uint4 *>(p + B::oV + off * B::kRow + q * 16));
+            w.pk = __ldg(reinterpret_cast<const uint16_t *>(p + B::oPK + (gr * kPage + off) * 2));
+            w.pv = __ldg(reinterpret_cast<const uint16_t *>(p + B::oPV + (gr * kPage + off) * 2));
+          }
+        }
+      };
+      static_assert(kTile == 2 * kPage && ITEMS % 2 == 0, "the first half of the items lies in a tile's first page");
+      look_up(0);
+      load(0);
+      look_up(1);
+      auto put = [&](unsigned char *tile, int k, const uint4 &codes, uint32_t param) {
+        const uint32_t z = (param & 15u) * 0x10001u;
+        const __half2 za = as_half2(z | 0x64006400u), zb = as_half2(z << 4 | 0x54005400u);
+        const __half2 s = as_half2((param & 0xFFF0u) * 0x10001u);
+        unsigned char *dst = tile + (octet[k] * C + 4 * q) * 128 + (lane & 7) * 16;
+        *reinterpret_cast<uint4 *>(dst) = decode(codes.x, s, za, zb);
+        *reinterpret_cast<uint4 *>(dst + 128) = decode(codes.y, s, za, zb);
+        *reinterpret_cast<uint4 *>(dst + 256) = decode(codes.z, s, za, zb);
+        *reinterpret_cast<uint4 *>(dst + 384) = decode(codes.w, s, za, zb);
+      };
+      for (int j = 0; j < tiles; ++j) {
+        const int st = j & 1;
+        Raw cur[ITEMS];
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k) {
-        const bool nan = (cur[k].pv & 0x7C00u) == 0x7C00u;
-        put(smem + Y::oV + st * Y::kTileBytes, k, cur[k].v, nan ? 0u : cur[k].pv);
+        for (int k = 0; k < ITEMS; ++k) cur[k] = raw[k];
+        if (j + 1 < tiles) {
+          load(j + 1);
+          look_up(j + 2);
+        }
+        if (j >= 2 && !__all_sync(0xffffffffu, wait(&bars->kempty[st], ((j >> 1) & 1) ^ 1, abort_))) break;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+          put(smem + Y::oK + st * Y::kTileBytes, k, cur[k].k, cur[k].pk);
+          // Values that stand for NaN become zeros (0 times NaN must not count) and are noted for
+          // the rows that see them, with the tile's scores.  Four tiles' notes: the values of the
+          // tile before this one went to a stage whose tile, three before, every row was done with.
+          const uint32_t bits = __ballot_sync(0xffffffffu, (cur[k].pv & 0x7C00u) == 0x7C00u);
+          if ((lane & 7) == 0 && q * 32 % kGrp == 0)
+            smem[Y::oLost + ((j & 3) * G + gr) * 16 + octet[k]] = (unsigned char)(bits >> lane);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->kfull[st]);
+        if (j >= 2 && !__all_sync(0xffffffffu, wait(&bars->vempty[st], ((j >> 1) & 1) ^ 1, abort_))) break;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+          const bool nan = (cur[k].pv & 0x7C00u) == 0x7C00u;
+          put(smem + Y::oV + st * Y::kTileBytes, k, cur[k].v, nan ? 0u : cur[k].pv);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->vfull[st]);
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->vfull[st]);
-    }
     }
   } else {
     registers_down<kMmaRegs>();
     if (work && warp == kMmaWarp && lane == 0 && tiles > 0) {
-    // ======================================================== MMA
-    const uint32_t idS = idesc_f16_f32(kTile, kTile), idO = idesc_f16_f32(kTile, D) | (1u << 16);  // V: MN-major
-    const uint32_t sQ = smem_u32(smem + Y::oQ), sK = smem_u32(smem + Y::oK), sV = smem_u32(smem + Y::oV);
-    // a step is 16 dimensions (two core matrices of a row group) or 16 tokens (two row groups)
-    auto scores = [&](int i, int st) {
-      const uint64_t q = smem_desc(sQ + i * Y::kTileBytes, 128, C * 128);
-      const uint64_t k = smem_desc(sK + st * Y::kTileBytes, 128, C * 128);
+      // ======================================================== MMA
+      const uint32_t idS = idesc_f16_f32(kTile, kTile), idO = idesc_f16_f32(kTile, D) | (1u << 16);  // V: MN-major
+      const uint32_t sQ = smem_u32(smem + Y::oQ), sK = smem_u32(smem + Y::oK), sV = smem_u32(smem + Y::oV);
+      // a step is 16 dimensions (two core matrices of a row group) or 16 tokens (two row groups)
+      auto scores = [&](int i, int st) {
+        const uint64_t q = smem_desc(sQ + i * Y::kTileBytes, 128, C * 128);
+        const uint64_t k = smem_desc(sK + st * Y::kTileBytes, 128, C * 128);
 #pragma unroll
-      for (int s4 = 0; s4 < D / 64; ++s4)
-        mma4_smemA<16>(tmem + i * kTile, q + s4 * 64, k + s4 * 64, idS, s4 > 0);
-      mma_commit(&bars->s[i]);
-    };
-    auto values = [&](int i, int j) {
-      const uint64_t v = smem_desc(sV + (j & 1) * Y::kTileBytes, C * 128, 128);
+        for (int s4 = 0; s4 < D / 64; ++s4)
+          mma4_smemA<16>(tmem + i * kTile, q + s4 * 64, k + s4 * 64, idS, s4 > 0);
+        mma_commit(&bars->s[i]);
+      };
+      auto values = [&](int i, int j) {
+        const uint64_t v = smem_desc(sV + (j & 1) * Y::kTileBytes, C * 128, 128);
 #pragma unroll
-      for (int s4 = 0; s4 < 2; ++s4)
-        mma4_tmemA<2 * C * 8>(tmem + 2 * kTile + i * D, tmem + i * kTile + s4 * 32, v + s4 * (4 * 2 * C * 8), idO,
-                              j > 0 || s4 > 0);
-    };
-    const int n0 = T.tiles[0], n1 = T.tiles[1];
-    bool ok = wait(&bars->q, 0, abort_) && wait(&bars->kfull[0], 0, abort_);
-    if (ok) {
-      tc_fence_after();
-      if (n0 > 0) scores(0, 0);
-      if (n1 > 0) scores(1, 0);
-      mma_commit(&bars->kempty[0]);
-    }
-    for (int j = 0; j < tiles && ok; ++j) {
-      const int st = j & 1, nx = (j + 1) & 1;
-      if (!(ok = wait(&bars->vfull[st], (j >> 1) & 1, abort_))) break;
-      for (int i = 0; i < 2 && ok; ++i) {
-        const int n = i ? n1 : n0;
-        if (j < n) {
-          if (!(ok = wait(&bars->p[i], j & 1, abort_))) break;
-          tc_fence_after();
-          values(i, j);
-          if (j + 1 == n) mma_commit(&bars->o[i]);
-        }
-        if (i == 1) mma_commit(&bars->vempty[st]);
-        if (j + 1 < tiles) {
-          if (i == 0 && !(ok = wait(&bars->kfull[nx], ((j + 1) >> 1) & 1, abort_))) break;
-          tc_fence_after();
-          if (j + 1 < n) scores(i, nx);
-          if (i == 1) mma_commit(&bars->kempty[nx]);
+        for (int s4 = 0; s4 < 2; ++s4)
+          mma4_tmemA<2 * C * 8>(tmem + 2 * kTile + i * D, tmem + i * kTile + s4 * 32, v + s4 * (4 * 2 * C * 8), idO,
+                                j > 0 || s4 > 0);
+      };
+      const int n0 = T.tiles[0], n1 = T.tiles[1];
+      bool ok = wait(&bars->q, 0, abort_) && wait(&bars->kfull[0], 0, abort_);
+      if (ok) {
+        tc_fence_after();
+        if (n0 > 0) scores(0, 0);
+        if (n1 > 0) scores(1, 0);
+        mma_commit(&bars->kempty[0]);
+      }
+      for (int j = 0; j < tiles && ok; ++j) {
+        const int st = j & 1, nx = (j + 1) & 1;
+        if (!(ok = wait(&bars->vfull[st], (j >> 1) & 1, abort_))) break;
+        for (int i = 0; i < 2 && ok; ++i) {
+          const int n = i ? n1 : n0;
+          if (j < n) {
+            if (!(ok = wait(&bars->p[i], j & 1, abort_))) break;
+            tc_fence_after();
+            values(i, j);
+            if (j + 1 == n) mma_commit(&bars->o[i]);
+          }
+          if (i == 1) mma_commit(&bars->vempty[st]);
+          if (j + 1 < tiles) {
+            if (i == 0 && !(ok = wait(&bars->kfull[nx], ((j + 1) >> 1) & 1, abort_))) break;
+            tc_fence_after();
+            if (j + 1 < n) scores(i, nx);
+            if (i == 1) mma_commit(&bars->kempty[nx]);
+          }
         }
       }
-    }
     }
   }
   __syncwarp();

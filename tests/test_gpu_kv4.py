@@ -138,6 +138,57 @@ def test_many_queries(tq, D, group, dtype, causal, window):
     run_attention(tq, lengths, n, 2, group, D, dtype, causal=causal, window=window, seed=7)
 
 
+@pytest.mark.parametrize("D,heads,group,dtype", [(128, 4, 8, "fp16"), (64, 8, 4, "fp16"), (128, 8, 5, "bf16"),
+                                                 (64, 2, 19, "bf16"), (128, 32, 1, "fp16")])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 90)])
+def test_enough_rows_for_the_tile_kernel(tq, D, heads, group, dtype, causal, window):
+    """Over 6000 query rows: prompts go to the kernel that decodes whole tiles,
+    the single queries and the few among them do not."""
+    lengths, n = [333, 130, 257, 40, 63, 200], [150, 130, 1, 33, 7, 2]
+    run_attention(tq, lengths, n, heads, group, D, dtype, causal=causal, window=window, seed=17)
+
+
+def test_tile_kernel_edges(tq):
+    # positions below zero, empty sequences and ranges, lengths around tiles of 128
+    run_attention(tq, [2, 0, 100, 5], [200, 2, 0, 260], 2, 8, 128, seed=3)
+    run_attention(tq, [2, 0, 100, 5], [200, 2, 0, 260], 4, 4, 64, seed=4, causal=False)
+    run_attention(tq, [128, 256, 129, 127, 384], [128, 64, 65, 63, 1], 4, 8, 128, seed=5)
+    run_attention(tq, [2000, 700], [60, 150], 4, 8, 128, seed=6, window=257)
+    # sharp, flat, growing and shrinking scores
+    for i, kw in enumerate((dict(qscale=12.0), dict(qscale=1e-4), dict(scale=0.0), dict(scale=-0.2), dict(qscale=40.0))):
+        run_attention(tq, [700, 300], [100, 140], 4, 8, 128, seed=24 + i, **kw)
+    run_attention(tq, [100, 200, 300], [60, 190], 4, 8, 128, slots=[1, 1], pad=8, seed=33)
+
+
+def test_more_prompts_than_the_longest_first_order_sorts(tq):
+    # over 32 sequences the blocks go sequence by sequence
+    lengths = [50 + 3 * i for i in range(40)]
+    run_attention(tq, lengths, [20 + (i % 3) * 15 for i in range(40)], 2, 4, 64, seed=9)
+
+
+def test_tile_kernel_keeps_what_is_not_a_number_to_its_rows(tq):
+    """As below for the kernel of few rows; here the row's own position also
+    decides whether it sees the token that stands for NaN."""
+    import torch
+    D, heads, group = 128, 4, 8
+    n, L = 220, 300
+    for value in (False, True):
+        c, data, table, length, refs = make(tq, [L], heads, D, seed=62)
+        at = PAGE * D + (2 * PAGE * 2 if value else 0) + 2 * (1 * PAGE + 200 % PAGE)  # group 1 of token 200, head 1
+        data[1, table[0, 200 // PAGE], 1, at], data[1, table[0, 200 // PAGE], 1, at + 1] = 0xF0, 0x7F
+        q = dev(np.random.default_rng(1).standard_normal((n, heads * group, D)).astype(np.float16))
+        q[5, 3, 0] = float("nan")
+        args = (c, 1, i32([0]), i32([0, n]))
+        clean = tq.tq_kv4_attention(q, *args).float().cpu().numpy()
+        c.data.copy_(dev(data))
+        out = tq.tq_kv4_attention(q, *args).float().cpu().numpy()
+        bad = np.zeros(out.shape, bool)
+        bad[200 - (L - n):, group:2 * group, 64 if value else 0:] = True  # rows from position 200 on
+        bad[5, 3] = True
+        assert np.isnan(out[bad]).all()
+        assert np.isfinite(out[~bad]).all() and np.array_equal(out[~bad], clean[~bad])
+
+
 def test_more_queries_than_tokens_and_empty_sequences(tq):
     # positions below zero see nothing: zeros and lse -inf; an empty sequence
     # and an empty range are fine anywhere in the list
