@@ -2,8 +2,10 @@
 // tq_kv4_read; format in include/tq.h).
 //
 // Eight lanes hold a group of 64 dimensions, eight values each: 16 bytes in,
-// the group's extremes by three shuffles, 4 bytes of codes out.  Bound by
-// memory: a value moves 2 bytes in and a little over half a byte out.
+// the group's extremes by three shuffles, 4 bytes of codes out.  A value moves 2
+// bytes in and a little over half a byte out (or the reverse): 4600 tokens of 8
+// heads of 128 in and out again 28 us, where the bytes alone take 12; appending is
+// bound by its instructions (about 150 for eight values), reading by its stores.
 #include "tq_kv4.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -24,7 +26,7 @@ __device__ __forceinline__ float to_float(uint16_t b) {
 // quotient that is not half way between integers is at least 2^-14 from there,
 // and one that is comes out of x r within 2^-18 of it.  Rounding to multiples of
 // 2^-15 puts the second kind back on the half and leaves the first on its side.
-// (Dividing takes 26 us instead of 12 for 2000 tokens of a prompt.)
+// (A division per value takes four times the instructions.)
 __device__ __forceinline__ float nearest(float x, float r) {
   const float q = __fadd_rn(__fadd_rn(__fmul_rn(x, r), 384.0f), -384.0f);
   return __fadd_rn(__fadd_rn(q, 12582912.0f), -12582912.0f);
@@ -90,7 +92,8 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
       // the integer from the low bits of 2^23 + c: a conversion would take a slower pipe
-      codes |= (__float_as_uint(__fadd_rn(fminf(fmaxf(nearest(x[i], r) + z, 0.0f), 15.0f), 8388608.0f)) & 15u) << (4 * i);
+      codes |= (__float_as_uint(__fadd_rn(fminf(fmaxf(nearest(x[i], r) + z, 0.0f), 15.0f), 8388608.0f)) & 15u)
+               << (4 * i);
   }
   if (!there) return;
   const int w = where[t];
@@ -133,8 +136,8 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t c = (codes >> (4 * i) & 0x000F000Fu) | 0x64006400u, za = z | 0x64006400u;
-      const __half2 d = __hmul2(__hsub2(*reinterpret_cast<const __half2 *>(&c), *reinterpret_cast<const __half2 *>(&za)),
-                                *reinterpret_cast<const __half2 *>(&sc));
+      const __half2 n = __hsub2(*reinterpret_cast<const __half2 *>(&c), *reinterpret_cast<const __half2 *>(&za));
+      const __half2 d = __hmul2(n, *reinterpret_cast<const __half2 *>(&sc));
       v[i] = *reinterpret_cast<const uint32_t *>(&d);
     }
 #pragma unroll
@@ -188,8 +191,8 @@ tq_status tq_kv4_append(const tq_kv4_cache *c, int32_t layer, int32_t tokens, in
   const bool vec = aligned_to(k, 16) && aligned_to(v, 16) && k_stride % 8 == 0 && v_stride % 8 == 0;
   const Rows in = {k, v, k_stride, v_stride};
   auto go = [&](auto kern) {
-    return from_cuda(launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, (uint32_t)items, in, where,
-                                      d_status));
+    return from_cuda(launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, (uint32_t)items, in,
+                                      where, d_status));
   };
   const bool bf = dtype == TQ_BF16;
   if (c->dim == 128) {
@@ -212,8 +215,8 @@ tq_status tq_kv4_read(const tq_kv4_cache *c, int32_t layer, int32_t tokens, int3
   unsigned grid;
   if (!grid_of(items, c->dim, &grid)) return TQ_ERR_SHAPE;
   auto go = [&](auto kern) {
-    return from_cuda(
-        launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, (uint32_t)items, where, k, v, d_status));
+    return from_cuda(launch_dependent(kern, dim3(grid), kThreads, (cudaStream_t)stream, *c, layer, (uint32_t)items,
+                                      where, k, v, d_status));
   };
   if (c->dim == 128) return dtype == TQ_BF16 ? go(read_kernel<128, true>) : go(read_kernel<128, false>);
   return dtype == TQ_BF16 ? go(read_kernel<64, true>) : go(read_kernel<64, false>);

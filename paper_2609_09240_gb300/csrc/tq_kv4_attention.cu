@@ -17,8 +17,9 @@
 //   * fp16 queries enter as they are; bf16 ones as fp16 times a power of two per
 //     row (their largest value in 2^10 .. 2^11), which loses nothing.
 //   * P is rounded to fp16, once.  Its scale: exp2 of the score less the running
-//     maximum, plus 29 less the largest exponent of s so far, puts the largest P
-//     just below 2^15; everything accumulated shares that factor.
+//     maximum, plus 23 less the largest exponent of s so far, puts a P at the
+//     maximum just below 2^9, so that the maximum may fall behind by a factor of
+//     2^6 before the sums are rescaled; everything accumulated shares that factor.
 //
 // Work split.  A unit is one page (64 tokens) of one K/V head for one tile of
 // query rows; a sequence's units lie in a row, sequences one after another.
@@ -148,6 +149,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 constexpr float kInf = std::numeric_limits<float>::infinity();
+constexpr int kTop = 23;
+constexpr float kGrow = 6.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // A partial result: D values of each row, then the logarithms that the values
@@ -340,14 +343,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
   uint32_t qf[NT][G][8];
   float F[NT][2];  // score factors of columns 2 j, 2 j + 1
   int begin[NT][2], end[NT][2], some_begin = 0, all_end = 0;
-  float O[NT][G][4][4], mx[NT][2], l[NT][2];
+  float O[NT][G][4][4], mx[NT][2], high[NT][2], l[NT][2];
   int E = 0;
   int64_t seg_begin = 0;
   auto clear = [&]() {
     E = 0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      mx[t][0] = mx[t][1] = -kInf;
+      mx[t][0] = mx[t][1] = high[t][0] = high[t][1] = -kInf;
       l[t][0] = l[t][1] = 0.0f;
 #pragma unroll
       for (int gr = 0; gr < G; ++gr)
@@ -392,7 +395,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
       for (int gr = 0; gr < G; ++gr)
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          const uint4 r = there ? __ldg(reinterpret_cast<const uint4 *>(q + gr * kGrp + 8 * v)) : make_uint4(0, 0, 0, 0);
+          const uint4 r =
+              there ? __ldg(reinterpret_cast<const uint4 *>(q + gr * kGrp + 8 * v)) : make_uint4(0, 0, 0, 0);
           const uint32_t rs[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -458,57 +462,60 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
           if (token(s, 1) >= L) vs[gr][s] &= 0x0000FFFFu;
         }
     }
-    // the largest exponent of a value scale
+    // the largest exponent of a value scale among the lane's tokens
     uint32_t top = 0;
 #pragma unroll
     for (int gr = 0; gr < G; ++gr) top = __vmaxu2(top, __vmaxu2(vs[gr][0] & 0x7C007C00u, vs[gr][1] & 0x7C007C00u));
-    top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16)) >> 10;
-    if (top == 31) {
-      // A group stands for NaN: in rows that see its token its dimensions are
-      // lost (here and now: an unseen token's 0 times NaN must not count), the
-      // others' scales stay.
-      top = 0;
+    top = max(top & 0xFFFFu, top >> 16) >> 10;
+    if (__any_sync(0xffffffffu, (int)top > E)) {
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (top == 31) {
+        // A group stands for NaN: in rows that see its token its dimensions are
+        // lost (here and now: an unseen token's 0 times NaN must not count), the
+        // others' scales stay.
+        top = 0;
 #pragma unroll
-      for (int gr = 0; gr < G; ++gr) {
-        bool lost[NT][2] = {};
+        for (int gr = 0; gr < G; ++gr) {
+          bool lost[NT][2] = {};
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            const uint32_t e = vs[gr][s] >> (16 * hi) & 0x7C00u;
-            if (e != 0x7C00u) {
-              top = max(top, e);
-              continue;
+            for (int hi = 0; hi < 2; ++hi) {
+              const uint32_t e = vs[gr][s] >> (16 * hi) & 0x7C00u;
+              if (e != 0x7C00u) {
+                top = max(top, e >> 10);
+                continue;
+              }
+              vs[gr][s] &= hi ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) lost[t][c] = lost[t][c] || sees(s, t, 2 * hi + c);
             }
-            vs[gr][s] &= hi ? 0x0000FFFFu : 0xFFFF0000u;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+          for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int c = 0; c < 2; ++c) lost[t][c] = lost[t][c] || sees(s, t, 2 * hi + c);
-          }
+            for (int c = 0; c < 2; ++c)
+              if (__ballot_sync(0xffffffffu, lost[t][c]) & (0x11111111u << j))
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            if (__ballot_sync(0xffffffffu, lost[t][c]) & (0x11111111u << j))
-#pragma unroll
-              for (int i = 0; i < 4; ++i) O[t][gr][i][c] = O[t][gr][i][2 + c] = kInf - kInf;
+                for (int i = 0; i < 4; ++i) O[t][gr][i][c] = O[t][gr][i][2 + c] = kInf - kInf;
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
       }
-      top = __reduce_max_sync(0xffffffffu, top) >> 10;
-    }
-    if ((int)top > E) {
-      const float f = __uint_as_float((uint32_t)(127 + E - (int)top) << 23);
-      E = (int)top;
+      if ((int)top > E) {
+        const float f = __uint_as_float((uint32_t)(127 + E - (int)top) << 23);
+        E = (int)top;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        l[t][0] *= f;
-        l[t][1] *= f;
+        for (int t = 0; t < NT; ++t) {
+          l[t][0] *= f;
+          l[t][1] *= f;
 #pragma unroll
-        for (int gr = 0; gr < G; ++gr)
+          for (int gr = 0; gr < G; ++gr)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) O[t][gr][i][k] *= f;
+              for (int i = 0; i < 4; ++i) O[t][gr][i][k] *= f;
+        }
       }
     }
     // scores (before the factor F) of the step's two tokens for columns 2 j, 2 j + 1
@@ -551,36 +558,46 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
           for (int k = 0; k < 4; ++k)
             if (!sees(s, t, k)) x[t][s][k] = -kInf;
     }
-    // running maximum; probabilities
+    // The reference of the exponentials follows the running maximum when that has
+    // grown by more than 2^kGrow: a look at the lane's own scores and a vote, where
+    // the columns' maxima would take six shuffles.
     bool grew = false;
-    float ref[NT][2], fac[NT][2];
+    float own[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float m = fmaxf(fmaxf(x[t][0][c], x[t][0][2 + c]), fmaxf(x[t][1][c], x[t][1][2 + c]));
-        m = fmaxf(m, mx[t][c]);
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        const float at = m == -kInf ? 0.0f : m * F[t][c];
-        fac[t][c] = exp2_fast(fmaf(mx[t][c], F[t][c], -at));
-        grew = grew || m > mx[t][c];
-        mx[t][c] = m;
-        ref[t][c] = (float)(29 - E) - at;
+        own[t][c] = fmaxf(fmaxf(x[t][0][c], x[t][0][2 + c]), fmaxf(x[t][1][c], x[t][1][2 + c]));
+        grew = grew || own[t][c] > high[t][c];
       }
     if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        l[t][0] *= fac[t][0];
-        l[t][1] *= fac[t][1];
 #pragma unroll
-        for (int gr = 0; gr < G; ++gr)
+        for (int c = 0; c < 2; ++c) {
+          float m = fmaxf(own[t][c], mx[t][c]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+          const float at = m == -kInf ? 0.0f : m * F[t][c];
+          const float f = exp2_fast(fmaf(mx[t][c], F[t][c], -at));
+          mx[t][c] = m;
+          high[t][c] = m + kGrow / F[t][c];
+          l[t][c] *= f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) O[t][gr][i][k] *= fac[t][k & 1];
+          for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              O[t][gr][i][c] *= f;
+              O[t][gr][i][2 + c] *= f;
+            }
+        }
       }
     }
+    float ref[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) ref[t][c] = (float)(kTop - E) - (mx[t][c] == -kInf ? 0.0f : mx[t][c] * F[t][c]);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -673,7 +690,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int r = 8 * t + 2 * j + c, row = tile * Part<D, NT>::kRows + r;
         const bool there = row < rows;
-        const float m = mx[t][c] == -kInf ? -kInf : mx[t][c] * F[t][c] - (float)(29 - E);
+        const float m = mx[t][c] == -kInf ? -kInf : mx[t][c] * F[t][c] - (float)(kTop - E);
         const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
         const int64_t token = T.q0[b] + (there ? row / g : 0);
         const int head = h * g + row % g;
