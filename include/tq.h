@@ -627,8 +627,7 @@ TQ_API tq_status tq_kv4_read(const tq_kv4_cache *c, int32_t layer, int32_t token
  * (causal != 0) and, with window > 0, j > its own - window; all of them with
  * causal = 0 (window must then be 0).  A token that sees nothing (a position
  * below 0) gets zeros and lse -inf.  Products and sums are fp32; p is
- * rounded to fp16 (with the rounding's rest carried along where there are few
- * query rows) for its product with the values.
+ * rounded to fp16, once, for its product with the values.
  *   q: [tokens][q_heads][dim], token t's row from element t * q_stride on
  *   (a multiple of 8), 16-byte aligned; out the same with out_stride; lse:
  *   optional fp32 [tokens][q_heads], the natural logarithm of the sum;
@@ -674,8 +673,10 @@ TQ_API tq_status tq_w4_quantize(int32_t N, int32_t K, const uint16_t *W, uint8_t
 TQ_API tq_status tq_w4_dequantize(int32_t N, int32_t K, const tq_w4_weight *w, uint16_t *out, void *stream);
 /* y = x W^T: x fp16 [M][K] (16-byte aligned), y fp16 [M][N] (tq_w4_linear_f32out:
  * fp32).  M >= 1.  The codes are multiplied as they are and the scales and
- * minima applied in fp32, so no weight is rounded.  Workspace:
- * tq_w4_workspace_bytes(M, N, K) bytes, 256-byte aligned, overwritten. */
+ * minima applied in fp32, so no weight is rounded.  More than 8 to 32 tokens
+ * (as many as fit a block's shared memory) take several passes over the weights:
+ * this is the product of a decode step, not of a long prompt.  Workspace:
+ * tq_w4_workspace_bytes(M, N, K) bytes, 256-byte aligned. */
 TQ_API size_t tq_w4_workspace_bytes(int32_t M, int32_t N, int32_t K);
 TQ_API tq_status tq_w4_linear(int32_t M, int32_t N, int32_t K, const tq_w4_weight *w, const uint16_t *x, uint16_t *y,
                               void *workspace, size_t workspace_bytes, void *stream);

@@ -21,14 +21,15 @@
 //                      the tensor cores work for the other
 // Tensor memory: S (P in its first half) of both tiles 2 x 128 columns, O 2 x D.
 // K tiles are K-major, V tiles the same bytes read MN-major (tokens are the
-// contraction there), in core matrices of 8 tokens x 16 bytes, unswizzled.
+// contraction there), in core matrices of 8 tokens x 16 bytes, unswizzled.  The
+// dimensions of a code word decode in the order 0 4 1 5 2 6 3 7; Q is stored in
+// that order and O read back from it.
+//
 // Measured (three prompts of 1223 to 1975 tokens, 5500 to 6000 keys, 32 query heads
 // on 8 of 128 dimensions): 357 us, 1050 TFLOP/s.  Of the 2.2 us per 128 keys the
 // MMAs take 0.87 (the scores' at 55 % of their rate: both operands come from
 // shared memory), the rest is the softmax's chain of a tile, which the other tile's
-// MMAs do not cover; without decoding it would be 329 us.  The
-// dimensions of a code word decode in the order 0 4 1 5 2 6 3 7; Q is stored in
-// that order and O read back from it.
+// MMAs do not cover; without decoding it would be 329 us.
 #include <cmath>
 #include <limits>
 

@@ -263,6 +263,29 @@ def test_what_is_not_a_number_stays_in_its_rows(tq):
         assert np.isfinite(out[~bad]).all() and np.array_equal(out[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("group_of_dims", [0, 1])
+def test_values_that_stand_for_nan_spoil_their_dimensions(tq, group_of_dims):
+    """Few rows: a NaN group among the values, seen by some of the queries only."""
+    D, heads = 128, 2
+    for n, window in ((1, 0), (3, 0), (6, 100)):
+        c, data, table, length, refs = make(tq, [300], heads, D, seed=63)
+        for tok in (120, 298):
+            at = PAGE * D + 2 * PAGE * 2 + 2 * (group_of_dims * PAGE + tok % PAGE)
+            data[1, table[0, tok // PAGE], 1, at], data[1, table[0, tok // PAGE], 1, at + 1] = 0xF5, 0x7F
+        q = dev(np.random.default_rng(1).standard_normal((n, 8, D)).astype(np.float16))
+        args = dict(max_q=n, window=window)
+        clean = tq.tq_kv4_attention(q, c, 1, i32([0]), i32([0, n]), **args).float().cpu().numpy()
+        c.data.copy_(dev(data))
+        out = tq.tq_kv4_attention(q, c, 1, i32([0]), i32([0, n]), **args).float().cpu().numpy()
+        bad = np.zeros(out.shape, bool)
+        for i in range(n):
+            pos = 300 - n + i
+            if pos >= 298 or not window:  # 298 in sight, or 120 (never inside the window)
+                bad[i, 4:, 64 * group_of_dims:64 * group_of_dims + 64] = True
+        assert np.isnan(out[bad]).all()
+        assert np.isfinite(out[~bad]).all() and np.array_equal(out[~bad], clean[~bad])
+
+
 def test_bad_lists_are_reported_and_harmless(tq):
     import torch
     for T0 in (1, 80):
