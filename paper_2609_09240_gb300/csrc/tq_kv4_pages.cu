@@ -116,6 +116,8 @@ inline ExtendWs extend_ws(int32_t *w, int slots, int count, int tokens) {
   return e;
 }
 
+constexpr int kNearList = 2048;
+
 // One block: checks the list, counts the pages each entry needs, finds them,
 // writes tables, counts and lengths.
 __global__ void __launch_bounds__(kPlanThreads)
@@ -124,6 +126,9 @@ __global__ void __launch_bounds__(kPlanThreads)
                        uint32_t *d_status) {
   __shared__ RankScratch sm;
   __shared__ int bad;
+  __shared__ int32_t near_off[kNearList + 1];
+  // searched once per page: in shared memory where the list fits
+  int32_t *need_off = count <= kNearList ? near_off : ws.need_off;
   const int tid = threadIdx.x;
   if (tid == 0) bad = 0;
   grid_dep_wait();
@@ -168,7 +173,7 @@ __global__ void __launch_bounds__(kPlanThreads)
       const int64_t a = block_scan(n, sm.part, &tt), b = block_scan(np, sm.part, &tp);
       if (i < count) {
         if (tok + a <= tokens) indptr[i] = (int32_t)(tok + a);
-        ws.need_off[i] = (int32_t)((pg + b) & 0xffffffff);
+        need_off[i] = (int32_t)((pg + b) & 0xffffffff);
         ws.pair_off[i] = (int32_t)((pg + b) >> 32);
       }
       tok += tt;
@@ -194,18 +199,18 @@ __global__ void __launch_bounds__(kPlanThreads)
     return;
   }
   if (tid == 0) {
-    ws.need_off[count] = (int32_t)need;
+    need_off[count] = (int32_t)need;
     indptr[count] = tokens;
     ws.pairs[0] = (int32_t)(pg >> 32);
   }
   __syncthreads();
   for (int64_t r = tid; r < need; r += kPlanThreads) {
-    const int i = find_range(ws.need_off, count, (int)r);
+    const int i = find_range(need_off, count, (int)r);
     const int s = slots[i], page = ws.page[r];
     const int64_t L = c.length[s], n = counts[i];
     const int64_t have = (L + kPage - 1) / kPage, want = (L + n + kPage - 1) / kPage;
-    const int j = (int)(r - ws.need_off[i]);
-    const int copy = (int)(ws.need_off[i + 1] - ws.need_off[i] - (want - have));
+    const int j = (int)(r - need_off[i]);
+    const int copy = (int)(need_off[i + 1] - need_off[i] - (want - have));
     int32_t *row = c.table + (int64_t)s * c.max_pages;
     if (j < copy) {
       const int old = row[L / kPage], k = ws.pair_off[i];

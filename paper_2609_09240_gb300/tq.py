@@ -61,8 +61,8 @@ class tq_ew_problem(ctypes.Structure):
 
 
 class tq_kv4_cache(ctypes.Structure):
-    _fields_ = [("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
-                ("slots", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("data", ctypes.c_void_p),
+    _fields_ = [("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("slots", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("data", ctypes.c_void_p),
                 ("table", ctypes.c_void_p), ("length", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
 
 
@@ -803,6 +803,11 @@ def _rows(t, name, heads, dim):
 
 def _raw_stream(stream):
     """The stream's handle as a number (the current stream's for None)."""
+    if stream is None:
+        try:
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:
+            pass
     return _stream(stream).value or 0
 
 
@@ -825,7 +830,7 @@ class Kv4Cache:
         c.data, c.table = _want(data, "data", torch.uint8), _want(table, "table", torch.int32)
         c.length, c.refs = (_want(length, "length", torch.int32, (slots,)), _want(refs, "refs", torch.int32, (pages,)))
         self._struct, self._ref = c, ctypes.byref(c)
-        self._status = self.status.data_ptr()
+        self._status, self.device = self.status.data_ptr(), data.device
         self._ws, self._outgrown, self._sizes = {}, [], {}
 
     @classmethod
@@ -880,9 +885,10 @@ def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, wher
     st = _raw_stream(stream)
     ws, nws = cache._scratch(st, "tq_kv4_extend_workspace_bytes", n, tokens)
     i32 = torch.int32
-    _check((_lib or lib()).tq_kv4_extend(cache._ref, n, _want(slots, "slots", i32, (n,)), _want(counts, "counts", i32, (n,)),
-                               tokens, _want(indptr, "indptr", i32, (n + 1,)), _want(where, "where", i32, (tokens,)), ws,
-                               nws, cache._status, st), "tq_kv4_extend")
+    _check((_lib or lib()).tq_kv4_extend(
+        cache._ref, n, _want(slots, "slots", i32, (n,)), _want(counts, "counts", i32, (n,)), tokens,
+        _want(indptr, "indptr", i32, (n + 1,)), _want(where, "where", i32, (tokens,)), ws, nws, cache._status, st),
+        "tq_kv4_extend")
     return indptr, where
 
 
@@ -943,15 +949,23 @@ def tq_kv4_append(k, v, cache: Kv4Cache, layer: int, where, stream=None):
 
 def tq_kv4_read(cache: Kv4Cache, layer: int, where, dtype=torch.float16, k=None, v=None, stream=None):
     """The keys and values held at the places where[]: two [tokens][heads][dim] tensors."""
-    T = where.shape[0]
-    shape = (T, cache.heads, cache.dim)
-    k = torch.empty(shape, dtype=dtype, device=where.device) if k is None else k
-    v = torch.empty(shape, dtype=dtype, device=where.device) if v is None else v
     if dtype not in _KV_DTYPE:
         raise ValueError(f"expected fp16 or bf16, got {dtype}")
-    _check((_lib or lib()).tq_kv4_read(cache._ref, layer, T, _KV_DTYPE[dtype], _want(where, "where", torch.int32, (T,)),
-                             _want(k, "k", dtype, shape), _want(v, "v", dtype, shape), cache._status,
-                             _raw_stream(stream)), "tq_kv4_read")
+    T = where.shape[0]
+    shape = (T, cache.heads, cache.dim)
+    wp = _want(where, "where", torch.int32, (T,))
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        kp = k.data_ptr()
+    else:
+        kp = _want(k, "k", dtype, shape)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=cache.device)
+        vp = v.data_ptr()
+    else:
+        vp = _want(v, "v", dtype, shape)
+    _check((_lib or lib()).tq_kv4_read(cache._ref, layer, T, _KV_DTYPE[dtype], wp, kp, vp, cache._status,
+                                       _raw_stream(stream)), "tq_kv4_read")
     return k, v
 
 
@@ -963,21 +977,24 @@ def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, 
     decode step).  scale: 1 / sqrt(dim) if None.  lse: optional fp32
     [tokens][q_heads] output.  Returns out."""
     qp, qs = _rows(q, "q", None, cache.dim)
-    T, Hq = q.shape[0], q.shape[1]
+    T, Hq, dim = q.shape
+    dtype = q.dtype
     if out is None:
-        out = torch.empty((T, Hq, cache.dim), dtype=q.dtype, device=q.device)
-    op, os_ = _rows(out, "out", Hq, cache.dim)
-    if out.dtype != q.dtype or out.shape[0] != T:
-        raise ValueError("out and q differ in tokens or type")
+        out = torch.empty((T, Hq, dim), dtype=dtype, device=cache.device)
+        op, os_ = out.data_ptr(), Hq * dim
+    else:
+        op, os_ = _rows(out, "out", Hq, dim)
+        if out.dtype is not dtype or out.shape[0] != T:
+            raise ValueError("out and q differ in tokens or type")
     n = slots.shape[0]
-    max_q = T if max_q is None else min(int(max_q), T)
+    max_q = T if max_q is None or max_q > T else int(max_q)
     st = _raw_stream(stream)
     ws, nws = cache._scratch(st, "tq_kv4_attention_workspace_bytes", n, T, max_q, Hq)
     lp = None if lse is None else _want(lse, "lse", torch.float32, (T, Hq))
-    _check((_lib or lib()).tq_kv4_attention(cache._ref, layer, n, _want(slots, "slots", torch.int32, (n,)),
-                                  _want(indptr, "indptr", torch.int32, (n + 1,)), T, max_q, Hq, _KV_DTYPE[q.dtype], qp,
-                                  qs, cache.dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
-                                  int(window), op, os_, lp, ws, nws, cache._status, st), "tq_kv4_attention")
+    _check((_lib or lib()).tq_kv4_attention(
+        cache._ref, layer, n, _want(slots, "slots", torch.int32, (n,)), _want(indptr, "indptr", torch.int32, (n + 1,)),
+        T, max_q, Hq, _KV_DTYPE[dtype], qp, qs, dim ** -0.5 if scale is None else scale, causal, window, op, os_, lp,
+        ws, nws, cache._status, st), "tq_kv4_attention")
     return out
 
 
@@ -991,7 +1008,8 @@ class W4Weight:
         s.tiles = tiles.data_ptr()
         self._struct, self._ref = s, ctypes.byref(s)
         # the product needs no scratch memory; the argument has to be there
-        self._ws = workspace(256, tiles.device)
+        self._ws, self.device = workspace(256, tiles.device), tiles.device
+        self._scratch = self._ws.data_ptr()
 
     @classmethod
     def _new(cls, N, K, device):
@@ -1051,11 +1069,12 @@ def tq_w4_linear(x, w: W4Weight, y=None, ws=None, stream=None, f32=False):
     dt = torch.float32 if f32 else torch.float16
     xp = _want(x, "x", torch.float16, (M, w.K))
     if y is None:
-        y = torch.empty((M, w.N), dtype=dt, device=x.device)
-    if ws is None:
-        ws = w._ws
+        y = torch.empty((M, w.N), dtype=dt, device=w.device)
+        yp = y.data_ptr()
+    else:
+        yp = _want(y, "y", dt, (M, w.N))
+    wsp, nws = (w._scratch, 256) if ws is None else (_want(ws, "ws", torch.uint8), ws.numel())
     L = _lib or lib()
     fn = L.tq_w4_linear_f32out if f32 else L.tq_w4_linear
-    _check(fn(M, w.N, w.K, w._ref, xp, _want(y, "y", dt, (M, w.N)), _want(ws, "ws", torch.uint8), ws.numel(),
-              _raw_stream(stream)), "tq_w4_linear")
+    _check(fn(M, w.N, w.K, w._ref, xp, yp, wsp, nws, _raw_stream(stream)), "tq_w4_linear")
     return y
