@@ -6,6 +6,7 @@
 // bytes in and a little over half a byte out (or the reverse): 4600 tokens of 8
 // heads of 128 in and out again 28 us, where the bytes alone take 12; appending is
 // bound by its instructions (about 150 for eight values), reading by its stores.
+#include "tq_codes4.cuh"
 #include "tq_kv4.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -131,20 +132,15 @@ __global__ void __launch_bounds__(kThreads)
     const uint32_t p = *reinterpret_cast<const uint16_t *>(blk + (val ? B::oPV : B::oPK) +
                                                            (part / (kGrp / kPer) * kPage + off) * 2);
     // (1024 + c) - (1024 + z), times s: exact in fp16 (nibbles i and 4 + i together)
-    const uint32_t z = (p & 15u) * 0x10001u, sc = (p & 0xFFF0u) * 0x10001u;
+    const __half2 za = low_nibbles(p * 0x10001u), sc = as_half2((p & 0xFFF0u) * 0x10001u);
     uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t c = (codes >> (4 * i) & 0x000F000Fu) | 0x64006400u, za = z | 0x64006400u;
-      const __half2 n = __hsub2(*reinterpret_cast<const __half2 *>(&c), *reinterpret_cast<const __half2 *>(&za));
-      const __half2 d = __hmul2(n, *reinterpret_cast<const __half2 *>(&sc));
-      v[i] = *reinterpret_cast<const uint32_t *>(&d);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = as_bits(__hmul2(__hsub2(low_nibbles(codes >> (4 * i)), za), sc));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t h = __byte_perm(v[2 * (i & 1)], v[2 * (i & 1) + 1], i < 2 ? 0x5410 : 0x7632);
       if (BF16) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+        const float2 f = __half22float2(as_half2(h));
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out[i]) : "f"(f.y), "f"(f.x));
       } else {
         out[i] = h;

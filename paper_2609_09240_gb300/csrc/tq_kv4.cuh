@@ -54,11 +54,6 @@ inline tq_status from_cuda(cudaError_t e) { return e == cudaSuccess ? TQ_OK : TQ
 
 __device__ __forceinline__ void report(uint32_t *d_status, uint32_t bit) { atomicOr(d_status, bit); }
 
-// The 16 bits of a param: scale (low four bits clear) and zero.
-__device__ __forceinline__ float param_scale(uint32_t p) {
-  return __half2float(__ushort_as_half((unsigned short)(p & 0xFFF0u)));
-}
-__device__ __forceinline__ float param_zero(uint32_t p) { return (float)(p & 15u); }
 
 // Tokens of a slot as the kernels use it: 0 <= n <= max_pages * 64.
 __device__ __forceinline__ int clamp_length(const tq_kv4_cache &c, int n) {

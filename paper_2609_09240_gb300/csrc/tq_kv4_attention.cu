@@ -30,10 +30,10 @@
 // maximum and sum; runs that end inside a sequence leave a partial result that
 // attn_combine_kernel joins.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <limits>
 
+#include "tq_codes4.cuh"
 #include "tq_kv4_attention.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -43,8 +43,8 @@ namespace kv4 {
 
 // Warps of a block (one block per SM) for NT tiles of eight query rows, and the
 // blocks of 64 tokens that each has under way.  One tile leaves the registers
-// for twelve warps: 48 sequences of 1000 to 8000 tokens take 76 us with twelve
-// (two blocks each) and 80 with eight (three); two tiles spill with twelve, and
+// for twelve warps: 48 sequences of 1000 to 8000 tokens take 74 us with twelve
+// (two blocks each; 76 when eight with three took 80); two tiles spill with twelve, and
 // a few queries for each of 16 sequences take 18 us with eight and 21 with twelve.
 template <int D, int NT>
 struct Shape {
@@ -143,11 +143,6 @@ struct Runs {
   }
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr int kTop = 23;
 constexpr float kGrow = 6.0f;
@@ -204,19 +199,6 @@ struct Soft {
   }
 };
 
-__device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// The same onto zeros.
-__device__ __forceinline__ void mma_f16_first(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
-}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -227,30 +209,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// (w & mask) | bits in one instruction: with two constants the compiler would
-// take two, it keeps no more than one immediate in an instruction.
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
-  return r;
-}
-__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
-// 1024 + (64 +) the nibble at bits 0 (4) of both 16-bit halves.
-__device__ __forceinline__ __half2 low_nibbles(uint32_t w) { return as_half2(and_or(w, 0x000F000Fu, 0x64006400u)); }
-__device__ __forceinline__ __half2 high_nibbles(uint32_t w) { return as_half2(and_or(w, 0x00F000F0u, 0x54005400u)); }
-// c - z of nibble I of both 16-bit halves; za = 1024 + z, zb = 64 + z.
-template <int I>
-__device__ __forceinline__ uint32_t codes(uint32_t w, __half2 za, __half2 zb) {
-  const uint32_t n = I < 2 ? w : w >> 8;
-  const __half2 d = (I & 1) ? __hsub2(high_nibbles(n), zb) : __hsub2(low_nibbles(n), za);
-  return *reinterpret_cast<const uint32_t *>(&d);
-}
-// 1024 + z and 64 + z from the zeros in the low four bits of both halves.
-__device__ __forceinline__ void zeros(uint32_t zz, __half2 *za, __half2 *zb) {
-  *za = low_nibbles(zz);
-  *zb = high_nibbles(zz * 16u);
-}
-
 template <int D, int NT>
 struct Ring {
   static constexpr int kBytes = Shape<D, NT>::kWarps * Shape<D, NT>::kStages * Block<D>::kBytes;
@@ -818,23 +776,6 @@ __global__ void __launch_bounds__(Part<D, NT>::kRows *Part<D, NT>::kLanes)
       if (i + k < n) f.join(m[k], l[k], o[k]);
   }
   f.template write<D, BF16>(a, J.q0, J.row0 + r, J.h, lane);
-}
-
-// SMs of the current device (asked once per device).
-int sm_count() {
-  constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 152;
-  int n = known[dev].load(std::memory_order_relaxed);
-  if (!n) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-      (void)cudaGetLastError();
-      return 152;
-    }
-    known[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
 }
 
 inline size_t split_ws_bytes(int D, int NT) {

@@ -33,6 +33,7 @@
 #include <cmath>
 #include <limits>
 
+#include "tq_codes4.cuh"
 #include "tq_kv4_attention.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -117,19 +118,6 @@ template <int N>
 __device__ __forceinline__ void registers_down() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
-  return r;
-}
-__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
-__device__ __forceinline__ uint32_t as_bits(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
-
 // Four MMAs over successive steps of the contraction, in one piece: written one
 // by one, each waits for its descriptors' arithmetic (130 cycles between MMAs
 // that take 32).  acc: does the first add to what is there?
@@ -165,10 +153,10 @@ __device__ __forceinline__ void mma4_tmemA(uint32_t d, uint32_t a, uint64_t b, u
 // The eight values of a code word, dimensions 0 4 1 5 2 6 3 7.
 __device__ __forceinline__ uint4 decode(uint32_t w, __half2 s, __half2 za, __half2 zb) {
   const uint32_t v = w >> 8;
-  return make_uint4(as_bits(__hmul2(__hsub2(as_half2(and_or(w, 0x000F000Fu, 0x64006400u)), za), s)),
-                    as_bits(__hmul2(__hsub2(as_half2(and_or(w, 0x00F000F0u, 0x54005400u)), zb), s)),
-                    as_bits(__hmul2(__hsub2(as_half2(and_or(v, 0x000F000Fu, 0x64006400u)), za), s)),
-                    as_bits(__hmul2(__hsub2(as_half2(and_or(v, 0x00F000F0u, 0x54005400u)), zb), s)));
+  return make_uint4(as_bits(__hmul2(__hsub2(low_nibbles(w), za), s)),
+                    as_bits(__hmul2(__hsub2(high_nibbles(w), zb), s)),
+                    as_bits(__hmul2(__hsub2(low_nibbles(v), za), s)),
+                    as_bits(__hmul2(__hsub2(high_nibbles(v), zb), s)));
 }
 
 // What a block works on.

@@ -1,8 +1,7 @@
 // tq_w4.cu - 4-bit weights with group scales: packing, quantization and the
 // product with a few tokens' activations (formats and definitions in
 // include/tq.h).
-#include <atomic>
-
+#include "tq_codes4.cuh"
 #include "tq_kv4.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -133,34 +132,6 @@ __global__ void __launch_bounds__(256)
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kAhead = 3;
 
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
-  return r;
-}
-// c - 8 of nibble I of both 16-bit halves.
-template <int I>
-__device__ __forceinline__ uint32_t codes(uint32_t w) {
-  const uint32_t n = I < 2 ? w : w >> 8;
-  const uint32_t x = (I & 1) ? and_or(n, 0x00F000F0u, 0x54005400u) : and_or(n, 0x000F000Fu, 0x64006400u);
-  const uint32_t o = (I & 1) ? 0x54805480u : 0x64086408u;  // 72, 1032
-  const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&o));
-  return *reinterpret_cast<const uint32_t *>(&d);
-}
-__device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// The same onto zeros.
-__device__ __forceinline__ void mma_f16_first(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
-}
-
 // Shared memory: x in operand order ([group][4][token][4 lanes] 16 bytes), the
 // sums of x per group and token ([group][8 NT] floats), two parts per warp
 // ([16 rows][8 NT] floats each), 16 zero bytes for the tokens that are not there.
@@ -256,6 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   float Y[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) Y[t][0] = Y[t][1] = Y[t][2] = Y[t][3] = 0.0f;
+  const __half2 o16 = as_half2(0x64086408u), o4 = as_half2(0x54805480u);  // 1024 + 8, 64 + 8
   // the lane's operands: token 8 t + nr's, or zeros
   const unsigned char *xl[NT];
   int xstep[NT];
@@ -271,11 +243,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t p0 = v.p0, p1 = v.p1;
     if (more_units) load(v);
     float acc[NT][4];
-#define TQ_STEP(I, P, B0, B1, MMA)                                                             \
-  {                                                                                            \
-    const uint32_t A[4] = {codes<I>(wa[2 * P]), codes<I>(wb[2 * P]), codes<I>(wa[2 * P + 1]),  \
-                           codes<I>(wb[2 * P + 1])};                                           \
-    _Pragma("unroll") for (int t = 0; t < NT; ++t) MMA(acc[t], A, b[t].B0, b[t].B1);           \
+#define TQ_STEP(I, P, B0, B1, MMA)                                                                        \
+  {                                                                                                       \
+    const uint32_t A[4] = {codes<I>(wa[2 * P], o16, o4), codes<I>(wb[2 * P], o16, o4),                    \
+                           codes<I>(wa[2 * P + 1], o16, o4), codes<I>(wb[2 * P + 1], o16, o4)};           \
+    _Pragma("unroll") for (int t = 0; t < NT; ++t) MMA(acc[t], A, b[t].B0, b[t].B1);                      \
   }
 #define TQ_LOAD()                                                                              \
   _Pragma("unroll") for (int t = 0; t < NT; ++t) {                                             \
@@ -374,22 +346,6 @@ Pass pass_of(int M, int K) {
   if (M > 16 && m4 > m2 && m4 > 16) return {4, m4};
   if (M > 8 && m2 > m1) return {2, m2};
   return {1, m1};
-}
-
-int sm_count() {
-  constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 152;
-  int n = known[dev].load(std::memory_order_relaxed);
-  if (!n) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-      (void)cudaGetLastError();
-      return 152;
-    }
-    known[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
 }
 
 template <int NT, bool F32>

@@ -217,6 +217,14 @@ def test_rows_apart_slots_out_of_order_and_repeated_reads(tq):
     run_attention(tq, [100, 200, 300], [40, 90], 2, 4, 128, slots=[1, 1], pad=8, seed=33)
 
 
+def test_more_sequences_than_a_launch_takes(tq):
+    # lists are worked through 512 sequences at a time
+    lengths = [(7 * i) % 150 for i in range(1030)]
+    run_attention(tq, lengths, [1 if i % 9 else 0 for i in range(1030)], 1, 2, 64, seed=43, max_q=1)
+    lengths = [20 + (7 * i) % 100 for i in range(530)]
+    run_attention(tq, lengths, [20 if i in (3, 520) else 1 for i in range(530)], 2, 8, 64, seed=44, max_q=20)
+
+
 def test_small_max_q_costs_no_results(tq):
     run_attention(tq, [400, 90], [150, 1], 2, 4, 128, max_q=1, seed=41)
 
