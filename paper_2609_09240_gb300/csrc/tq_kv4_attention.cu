@@ -16,10 +16,14 @@
 // registers, where mma.sync takes its operands.
 //   * fp16 queries enter as they are; bf16 ones as fp16 times a power of two per
 //     row (their largest value in 2^10 .. 2^11), which loses nothing.
-//   * P is rounded to fp16, once.  Its scale: exp2 of the score less the running
-//     maximum, plus 23 less the largest exponent of s so far, puts a P at the
-//     maximum just below 2^9, so that the maximum may fall behind by a factor of
-//     2^6 before the sums are rescaled; everything accumulated shares that factor.
+//   * P is rounded to fp16, once.  Each row and group has a power of two of its
+//     own for it, which brings the largest p_t s_t that the row has met just below
+//     2^9: a group of small values beside one of large ones, or tokens of small
+//     values beside one of large ones that counts little, keep their bits (what
+//     is under 2^-22 of the row's and group's largest is rounded as a subnormal
+//     number).  A P that overflows shows in what is packed, and moves the row's
+//     references: the maximum may fall behind by a factor of 2^7 before the sums
+//     are rescaled.
 //
 // Work split.  A unit is one page (64 tokens) of one K/V head for one tile of
 // query rows; a sequence's units lie in a row, sequences one after another.
@@ -144,8 +148,9 @@ struct Runs {
 };
 
 constexpr float kInf = std::numeric_limits<float>::infinity();
-constexpr int kTop = 23;
-constexpr float kGrow = 6.0f;
+constexpr int kTop = 9;             // 2^kTop: where a row's and group's largest P is put
+constexpr float kFirst = -3.0e38f;  // the reference of rows that have seen nothing
+constexpr float kMost = 0x1p100f;   // of the sum, whose exponentials follow the first group's power of two
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // A partial result: D values of each row, then the logarithms that the values
@@ -207,6 +212,12 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// The larger magnitudes of two pairs (the signs mean nothing); NaN where either is NaN.
+__device__ __forceinline__ uint32_t larger_of(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 template <int D, int NT>
@@ -301,14 +312,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
   uint32_t qf[NT][G][8];
   float F[NT][2];  // score factors of columns 2 j, 2 j + 1
   int begin[NT][2], end[NT][2], some_begin = 0, all_end = 0;
-  float O[NT][G][4][4], mx[NT][2], high[NT][2], l[NT][2];
-  int E = 0;
+  // P = exp2((score - mx) F + up) s, times beside in group 1; l: the sum of the exponentials
+  float O[NT][G][4][4], mx[NT][2], up[NT][2], beside[NT][2], l[NT][2];
   int64_t seg_begin = 0;
   auto clear = [&]() {
-    E = 0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      mx[t][0] = mx[t][1] = high[t][0] = high[t][1] = -kInf;
+      mx[t][0] = mx[t][1] = kFirst;
+      up[t][0] = up[t][1] = 20.0f;
+      beside[t][0] = beside[t][1] = 1.0f;
       l[t][0] = l[t][1] = 0.0f;
 #pragma unroll
       for (int gr = 0; gr < G; ++gr)
@@ -372,17 +384,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
       int e = 0;
       if (BF16 && top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
       // a negative scale turns the queries' sign, none makes them zeros: F > 0
-      float up = BF16 ? __uint_as_float((uint32_t)(127 + e) << 23) : 1.0f;
-      up = a.scale < 0.0f ? -up : a.scale == 0.0f ? 0.0f : up;
+      float by = BF16 ? __uint_as_float((uint32_t)(127 + e) << 23) : 1.0f;
+      by = a.scale < 0.0f ? -by : a.scale == 0.0f ? 0.0f : by;
 #pragma unroll
       for (int gr = 0; gr < G; ++gr)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          qf[t][gr][2 * i] = pack_f16(x[gr][i] * up, x[gr][4 + i] * up);
-          qf[t][gr][2 * i + 1] = pack_f16(x[gr][8 + i] * up, x[gr][12 + i] * up);
+          qf[t][gr][2 * i] = pack_f16(x[gr][i] * by, x[gr][4 + i] * by);
+          qf[t][gr][2 * i + 1] = pack_f16(x[gr][8 + i] * by, x[gr][12 + i] * by);
         }
       const float Fr =
-          a.scale == 0.0f ? 1.0f : fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-37f);
+          a.scale == 0.0f ? 1.0f : fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-30f);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         F[t][c] = __shfl_sync(0xffffffffu, Fr, 4 * (2 * j + c));
@@ -419,62 +431,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
           if (token(s, 0) >= L) vs[gr][s] &= 0xFFFF0000u;
           if (token(s, 1) >= L) vs[gr][s] &= 0x0000FFFFu;
         }
-    }
-    // the largest exponent of a value scale among the lane's tokens
-    uint32_t top = 0;
-#pragma unroll
-    for (int gr = 0; gr < G; ++gr) top = __vmaxu2(top, __vmaxu2(vs[gr][0] & 0x7C007C00u, vs[gr][1] & 0x7C007C00u));
-    top = max(top & 0xFFFFu, top >> 16) >> 10;
-    if (__any_sync(0xffffffffu, (int)top > E)) {
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (top == 31) {
-        // A group stands for NaN: in rows that see its token its dimensions are
-        // lost (here and now: an unseen token's 0 times NaN must not count), the
-        // others' scales stay.
-        top = 0;
-#pragma unroll
-        for (int gr = 0; gr < G; ++gr) {
-          bool lost[NT][2] = {};
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-              const uint32_t e = vs[gr][s] >> (16 * hi) & 0x7C00u;
-              if (e != 0x7C00u) {
-                top = max(top, e >> 10);
-                continue;
-              }
-              vs[gr][s] &= hi ? 0x0000FFFFu : 0xFFFF0000u;
-#pragma unroll
-              for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) lost[t][c] = lost[t][c] || sees(s, t, 2 * hi + c);
-            }
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (__ballot_sync(0xffffffffu, lost[t][c]) & (0x11111111u << j))
-#pragma unroll
-                for (int i = 0; i < 4; ++i) O[t][gr][i][c] = O[t][gr][i][2 + c] = kInf - kInf;
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-      }
-      if ((int)top > E) {
-        const float f = __uint_as_float((uint32_t)(127 + E - (int)top) << 23);
-        E = (int)top;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          l[t][0] *= f;
-          l[t][1] *= f;
-#pragma unroll
-          for (int gr = 0; gr < G; ++gr)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) O[t][gr][i][k] *= f;
-        }
-      }
     }
     // scores (before the factor F) of the step's two tokens for columns 2 j, 2 j + 1
     float x[NT][2][4];
@@ -516,55 +472,129 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
           for (int k = 0; k < 4; ++k)
             if (!sees(s, t, k)) x[t][s][k] = -kInf;
     }
-    // The reference of the exponentials follows the running maximum when that has
-    // grown by more than 2^kGrow: a look at the lane's own scores and a vote, where
-    // the columns' maxima would take six shuffles.
-    bool grew = false;
-    float own[NT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        own[t][c] = fmaxf(fmaxf(x[t][0][c], x[t][0][2 + c]), fmaxf(x[t][1][c], x[t][1][2 + c]));
-        grew = grew || own[t][c] > high[t][c];
-      }
-    if (__any_sync(0xffffffffu, grew)) {
+    // P, packed as the values' operands, and the sums; again after a reference has moved
+    uint32_t pf[G][NT][2][2];
+    float sum[NT][2];
+    for (bool moved = false;;) {
+      float p[NT][2][4];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
+        sum[t][0] = l[t][0];
+        sum[t][1] = l[t][1];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            p[t][s][k] = exp2_fast(fmaf(x[t][s][k] - mx[t][k & 1], F[t][k & 1], up[t][k & 1]));
+            sum[t][k & 1] += p[t][s][k];
+          }
+      }
+#pragma unroll
+      for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const float2 sc = __half22float2(as_half2(vs[gr][s] & 0xFFF0FFF0u));
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const float b0 = gr ? beside[t][0] : 1.0f, b1 = gr ? beside[t][1] : 1.0f;
+            pf[gr][t][s][0] = pack_f16(p[t][s][0] * sc.x * b0, p[t][s][1] * sc.x * b1);
+            pf[gr][t][s][1] = pack_f16(p[t][s][2] * sc.y * b0, p[t][s][3] * sc.y * b1);
+          }
+        }
+      // columns 2 j (low half) and 2 j + 1 with a P that is no finite number
+      uint32_t over[NT];
+      bool some = false;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        over[t] = pf[0][t][0][0];
+#pragma unroll
+        for (int i = 1; i < 4 * G; ++i) over[t] = larger_of(over[t], pf[i >> 2][t][i >> 1 & 1][i & 1]);
+        over[t] = ((over[t] & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+        some = some || over[t] != 0 || !(sum[t][0] + sum[t][1] <= kMost);
+      }
+      if (moved || !__any_sync(0xffffffffu, some)) break;
+      // A group stands for NaN: in rows that see its token its dimensions are
+      // lost (here and now: an unseen token's 0 times NaN must not count), the
+      // others' scales stay.
+      bool nan = false;
+#pragma unroll
+      for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) nan = nan || (((vs[gr][s] & 0x7C007C00u) + 0x04000400u) & 0x80008000u) != 0;
+      if (__any_sync(0xffffffffu, nan)) {
+#pragma unroll
+        for (int gr = 0; gr < G; ++gr) {
+          bool lost[NT][2] = {};
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              if ((vs[gr][s] >> (16 * hi) & 0x7C00u) != 0x7C00u) continue;
+              vs[gr][s] &= hi ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) lost[t][c] = lost[t][c] || sees(s, t, 2 * hi + c);
+            }
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              if (__ballot_sync(0xffffffffu, lost[t][c]) & (0x11111111u << j))
+#pragma unroll
+                for (int i = 0; i < 4; ++i) O[t][gr][i][c] = O[t][gr][i][2 + c] = kInf - kInf;
+        }
+        continue;
+      }
+      // The references of the columns concerned, of no others: a row's result does
+      // not depend on the rows beside it.
+      moved = true;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float m = fmaxf(own[t][c], mx[t][c]);
+          const bool mine = (over[t] >> (16 * c) & 0x8000u) != 0 || !(sum[t][c] <= kMost);
+          const bool move = (__ballot_sync(0xffffffffu, mine) & (0x11111111u << j)) != 0;
+          float m = fmaxf(fmaxf(x[t][0][c], x[t][0][2 + c]), fmaxf(x[t][1][c], x[t][1][2 + c]));
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-          const float at = m == -kInf ? 0.0f : m * F[t][c];
-          const float f = exp2_fast(fmaf(mx[t][c], F[t][c], -at));
-          mx[t][c] = m;
-          high[t][c] = m + kGrow / F[t][c];
-          l[t][c] *= f;
+          const float to = move ? fmaxf(m, mx[t][c]) : mx[t][c];
+          const float less = move ? exp2_fast((mx[t][c] - to) * F[t][c]) : 1.0f;
+          const float least = exp2_fast((m - to) * F[t][c]) * 0x1p-60f;
+          int now[G], was[G];
 #pragma unroll
-          for (int gr = 0; gr < G; ++gr)
+          for (int gr = 0; gr < G; ++gr) {
+            was[gr] = (int)up[t][c] + (gr ? (int)(__float_as_uint(beside[t][c]) >> 23) - 127 : 0);
+            float top = 0.0f;  // the largest p s among these tokens ...
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const float2 sc = __half22float2(as_half2(vs[gr][s] & 0x7FF07FF0u));
+              top = fmaxf(top, exp2_fast((x[t][s][c] - to) * F[t][c]) * sc.x);
+              top = fmaxf(top, exp2_fast((x[t][s][2 + c] - to) * F[t][c]) * sc.y);
+            }
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            // ... and of those before
+            top = fmaxf(fmaxf(top, least), exp2_fast((float)(kTop - was[gr])) * less);
+            now[gr] = move ? min(max(kTop - ((int)(__float_as_uint(top) + 0x7FFFFFu >> 23) - 127), -30), 80) : was[gr];
+            const float f = less * exp2_fast((float)(now[gr] - was[gr]));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               O[t][gr][i][c] *= f;
               O[t][gr][i][2 + c] *= f;
             }
+            if (gr == 0) l[t][c] *= f;
+          }
+          mx[t][c] = to;
+          up[t][c] = (float)now[0];
+          if (G > 1) beside[t][c] = __uint_as_float((uint32_t)(127 + now[G - 1] - now[0]) << 23);
         }
-      }
     }
-    float ref[NT][2];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) ref[t][c] = (float)(kTop - E) - (mx[t][c] == -kInf ? 0.0f : mx[t][c] * F[t][c]);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[t][s][k] = exp2_fast(fmaf(x[t][s][k], F[t][k & 1], ref[t][k & 1]));
-          l[t][k & 1] += x[t][s][k];
-        }
+    for (int t = 0; t < NT; ++t) {
+      l[t][0] = sum[t][0];
+      l[t][1] = sum[t][1];
+    }
     // values
 #pragma unroll
     for (int gr = 0; gr < G; ++gr) {
@@ -573,12 +603,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
       const uint2 za = *reinterpret_cast<const uint2 *>(zp), zb = *reinterpret_cast<const uint2 *>(zp + 16);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const float2 sc = __half22float2(as_half2(vs[gr][s] & 0xFFF0FFF0u));
         uint32_t bf[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          bf[t][0] = transpose8x8(pack_f16(x[t][s][0] * sc.x, x[t][s][1] * sc.x));
-          bf[t][1] = transpose8x8(pack_f16(x[t][s][2] * sc.y, x[t][s][3] * sc.y));
+          bf[t][0] = transpose8x8(pf[gr][t][s][0]);
+          bf[t][1] = transpose8x8(pf[gr][t][s][1]);
         }
         // the column pairs' tokens: those of rows 2 j, 2 j + 1, and of the rows 8 further on
         const unsigned char *vp = blk + B::oV + (16 * j + 4 * half + 2 * s) * B::kRow + gr * (kGrp / 2) + nr * 4;
@@ -648,17 +677,20 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int r = 8 * t + 2 * j + c, row = tile * Part<D, NT>::kRows + r;
         const bool there = row < rows;
-        const float m = mx[t][c] == -kInf ? -kInf : mx[t][c] * F[t][c] - (float)(kTop - E);
-        const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+        // a part's values and sum without the powers of two
+        const float by = __uint_as_float((uint32_t)(127 - (int)up[t][c]) << 23);
+        const float m = sum == 0.0f ? -kInf : mx[t][c] * F[t][c];
+        const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : by;
         const int64_t token = T.q0[b] + (there ? row / g : 0);
         const int head = h * g + row % g;
 #pragma unroll
         for (int gr = 0; gr < G; ++gr) {
+          const float inv_g = gr ? inv / beside[t][c] : inv;
           float o[8];  // dimensions 64 gr + 8 nr ..
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            o[i] = O[t][gr][i][c] * inv;
-            o[4 + i] = O[t][gr][i][2 + c] * inv;
+            o[i] = O[t][gr][i][c] * inv_g;
+            o[4 + i] = O[t][gr][i][2 + c] * inv_g;
           }
           if (!whole && there) {
             float4 *dst = reinterpret_cast<float4 *>(part + r * D + gr * kGrp + 8 * nr);
@@ -675,9 +707,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
         if (nr == 0 && there) {
           if (!whole) {
             part[Part<D, NT>::kRows * D + r] = m;
-            part[Part<D, NT>::kRows * (D + 1) + r] = sum;
+            part[Part<D, NT>::kRows * (D + 1) + r] = sum * by;
           } else if (a.lse) {
-            a.lse[token * a.q_heads + head] = sum == 0.0f ? -kInf : kLn2 * (m + log2f(sum));
+            a.lse[token * a.q_heads + head] = sum == 0.0f ? -kInf : kLn2 * (m - up[t][c] + log2f(sum));
           }
         }
       }

@@ -1,0 +1,107 @@
+"""Attention over the 4-bit K/V cache where the numbers span wide ranges: value
+scales, scores, windows and queries at the ends of what the formats hold, in
+the kernel for few query rows and in the one for many.  Tolerances as in
+test_gpu_kv4, except where a test derives its own."""
+import numpy as np
+import pytest
+
+from oracle import q4
+from test_gpu_kv4 import PAGE, check_attention, dev, i32, make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tq():
+    from paper_2609_09240_gb300 import tq
+    return tq
+
+
+def v_params(data, D):
+    """The params of the values: a view [..][D / 64][64] of the blocks' ends."""
+    at = PAGE * D + (D // 64) * PAGE * 2
+    return data[..., at:].view(np.uint16).reshape(data.shape[:-1] + (D // 64, PAGE))
+
+
+def scale_bits(exponent):
+    return int(np.float16(2.0 ** exponent).view(np.uint16))
+
+
+def attend(tq, c, q, slots, n, layer=0, **kw):
+    import torch
+    out = torch.full_like(q, float("nan"))
+    lse = torch.full(q.shape[:2], float("nan"), dtype=torch.float32, device="cuda")
+    tq.tq_kv4_attention(q, c, layer, i32(slots), i32(np.concatenate([[0], np.cumsum(n)])), out=out, lse=lse, **kw)
+    torch.cuda.synchronize()
+    c.check()
+    return out, lse
+
+
+def queries(rng, T, Hq, D, dtype, positive=False):
+    import torch
+    q = rng.standard_normal((T, Hq, D)).astype(np.float32)
+    return dev(np.abs(q) if positive else q).to({"fp16": torch.float16, "bf16": torch.bfloat16}[dtype])
+
+
+# ------------------------------------------------------------- value scales
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("large,small", [(0, 1), (1, 0)])
+@pytest.mark.parametrize("lengths,n,heads,group", [([500, 70], [1, 1], 2, 4), ([500, 70], [5, 3], 2, 4), ([9000], [2], 1, 3),
+                                                   ([330, 260], [170, 60], 4, 8)])
+def test_a_group_of_small_values_beside_large_ones(tq, dtype, large, small, lengths, n, heads, group):
+    """One group of a head's dimensions at 2^12, the other at 2^-16."""
+    D = 128
+    c, data, table, length, _ = make(tq, lengths, heads, D, seed=51, poison=False)
+    p = v_params(data, D)
+    for gr, e in ((large, 12), (small, -16)):
+        p[..., gr, :] = p[..., gr, :] & 15 | scale_bits(e)
+    c.data.copy_(dev(data))
+    q = queries(np.random.default_rng(52), sum(n), heads * group, D, dtype)
+    out, lse = attend(tq, c, q, range(len(n)), n)
+    check_attention(c, data, table, length, range(len(n)), n, heads, group, D, 0, q, out, lse, True, 0, D ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("far", [2.3, 4.6, 0.0])
+@pytest.mark.parametrize("at", [0, 130, 298])
+def test_a_token_of_large_values_that_counts_little(tq, D, dtype, far, at):
+    """Values of 2^12 at one token whose probability is about 2^-30 or 2^-60 of the
+    others' (far > 0) or ordinary, everything else at 2^-16; with at = 298 two of the
+    three queries do not see it."""
+    heads, group = 2, 4
+    c, data, table, length, _ = make(tq, [300], heads, D, seed=53, poison=False)
+    p = v_params(data, D)
+    p[...] = p & 15 | scale_bits(-16)
+    rng = np.random.default_rng(54)
+    for h in range(heads):
+        q4.store(data[0, table[0, at // PAGE], h], D, at % PAGE, np.full(D, -far * (128 / D) ** 0.5, np.float32),
+                 (rng.standard_normal(D) * 10000).astype(np.float32))
+    c.data.copy_(dev(data))
+    for n in (1, 3):
+        q = queries(rng, n, heads * group, D, dtype, positive=True)
+        out, lse = attend(tq, c, q, [0], [n])
+        check_attention(c, data, table, length, [0], [n], heads, group, D, 0, q, out, lse, True, 0, D ** -0.5, dtype)
+
+
+def test_zero_scales_and_growing_scores(tq):
+    """Groups whose values are all zero keep nothing of a row's references; scores
+    that grow along the sequence move them many times."""
+    D, heads, group = 128, 2, 4
+    rng = np.random.default_rng(55)
+    c, data, table, length, _ = make(tq, [700], heads, D, seed=56, poison=False)
+    ramp = np.linspace(0, 40, 700)
+    for h in range(heads):
+        for t in range(700):
+            v = rng.standard_normal(D).astype(np.float32) * 2.0 ** rng.integers(-14, 10)
+            v[:64] *= t % 3 > 0
+            v[64:] *= t > 350
+            q4.store(data[0, table[0, t // PAGE], h], D, t % PAGE,
+                     (rng.standard_normal(D) + ramp[t] / 10).astype(np.float32), v)
+    c.data.copy_(dev(data))
+    for n in (1, 4):
+        q = queries(rng, n, heads * group, D, "fp16", positive=True)
+        for kw in ({}, {"scale": -0.05}):
+            out, lse = attend(tq, c, q, [0], [n], **kw)
+            check_attention(c, data, table, length, [0], [n], heads, group, D, 0, q, out, lse, True, 0,
+                            kw.get("scale", D ** -0.5), "fp16")
