@@ -65,8 +65,7 @@ struct SeqTable {
 
 // Pages [p0, p1) that any query of the sequence sees.
 __device__ __forceinline__ void seq_pages(const AttnArgs &a, int L, int n, int *p0, int *np) {
-  const int first = a.window > 0 ? max(0, L - n - a.window + 1) : 0;
-  *p0 = first / kPage;
+  *p0 = first_seen(L - n, a.window) / kPage;
   *np = (L + kPage - 1) / kPage - *p0;
 }
 
@@ -353,7 +352,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
     const int row_lo = tile * 8 * NT, row_hi = min(row_lo + 8 * NT, rows) - 1;
     const int pos_lo = L - n + row_lo / g, pos_hi = L - n + row_hi / g;
     all_end = a.causal ? pos_lo + 1 : L;                             // every row sees the tokens before
-    some_begin = a.window > 0 ? max(0, pos_hi - a.window + 1) : 0;  // ... from here on
+    some_begin = first_seen(pos_hi, a.window);            // ... from here on
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int row = row_lo + 8 * t + nr;
@@ -401,7 +400,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
         const int rc = row_lo + 8 * t + 2 * j + c;
         const int pos = L - n + rc / g;
         end[t][c] = rc < rows ? (a.causal ? pos + 1 : L) : 0;
-        begin[t][c] = a.window > 0 ? pos - a.window + 1 : 0;
+        begin[t][c] = first_seen(pos, a.window);
       }
     }
     clear();

@@ -23,6 +23,13 @@ struct AttnArgs {
 cudaError_t launch_attn_prefill(const AttnArgs &a, bool bf16, cudaStream_t st);
 cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear);
 
+// The first position that a query at `pos` (below 0: before the sequence) sees;
+// a window may be as wide as its type.
+__device__ __forceinline__ int first_seen(int pos, int window) {
+  const int64_t at = (int64_t)pos - window + 1;
+  return window > 0 && at > 0 ? (int)at : 0;
+}
+
 // Two results in the output's type.
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {

@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
         T.row0 = tile * 2 * kTile;
         T.rows = min(n * g - T.row0, 2 * kTile);
         const int first = before + T.row0 / g;  // position of the first row
-        T.t0 = a.window > 0 ? max(0, first - a.window + 1) / kPage * kPage : 0;
+        T.t0 = first_seen(first, a.window) / kPage * kPage;
         for (int i = 0; i < 2; ++i) {
           const int r = min(T.rows, (i + 1) * kTile) - 1;  // the row tile's last row
           const int end = r < i * kTile ? 0 : a.causal ? before + (T.row0 + r) / g + 1 : T.L;
@@ -346,11 +346,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       mbar_arrive(&bars->q);
       // ---- what the row sees: [begin, end)
       const int pos = T.L - T.n + row / g;
-      const int end = !there ? 0 : a.causal ? pos + 1 : T.L, begin = a.window > 0 ? pos - a.window + 1 : 0;
+      const int end = !there ? 0 : a.causal ? pos + 1 : T.L, begin = first_seen(pos, a.window);
       // what every row of the tile sees
       const int pos_lo = T.L - T.n + (T.row0 + i * kTile) / g;
       const int pos_hi = T.L - T.n + (T.row0 + min(T.rows, (i + 1) * kTile) - 1) / g;
-      const int all_end = a.causal ? pos_lo + 1 : T.L, all_begin = a.window > 0 ? pos_hi - a.window + 1 : 0;
+      const int all_end = a.causal ? pos_lo + 1 : T.L, all_begin = first_seen(pos_hi, a.window);
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 (warp % 4) in the lane field
       const uint32_t tS = tmem + i * kTile + lanes, tO = tmem + 2 * kTile + i * D + lanes;
       float m = -kInf, l = 0.0f;  // the reference of the exponentials (a score before F) and the sum

@@ -105,3 +105,15 @@ def test_zero_scales_and_growing_scores(tq):
             out, lse = attend(tq, c, q, [0], [n], **kw)
             check_attention(c, data, table, length, [0], [n], heads, group, D, 0, q, out, lse, True, 0,
                             kw.get("scale", D ** -0.5), "fp16")
+
+
+# ------------------------------------------------------------------ windows
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30, 2 ** 31 - 64])
+@pytest.mark.parametrize("lengths,n,heads,group", [([2, 0, 100, 1], [9, 3, 4, 70], 2, 4), ([2, 0, 100, 1], [210, 70, 4, 99], 4, 8)])
+def test_windows_wider_than_any_sequence(tq, window, lengths, n, heads, group):
+    """More queries than tokens below the widest windows there are."""
+    D = 128
+    c, data, table, length, _ = make(tq, lengths, heads, D, seed=59)
+    q = queries(np.random.default_rng(60), sum(n), heads * group, D, "fp16")
+    out, lse = attend(tq, c, q, range(4), n, window=window)
+    check_attention(c, data, table, length, range(4), n, heads, group, D, 0, q, out, lse, True, window, D ** -0.5, "fp16")
