@@ -676,9 +676,12 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int r = 8 * t + 2 * j + c, row = tile * Part<D, NT>::kRows + r;
         const bool there = row < rows;
-        // a part's values and sum without the powers of two
-        const float by = __uint_as_float((uint32_t)(127 - (int)up[t][c]) << 23);
-        const float m = sum == 0.0f ? -kInf : mx[t][c] * F[t][c];
+        // A part's values and sum without the powers of two, and for the logarithm as
+        // it is rounded (from 2^30 on scores are equal or so far apart that only one
+        // counts, and equal ones round alike).
+        const float at = mx[t][c] * F[t][c], m = sum == 0.0f ? -kInf : at;
+        const float rest = fabsf(at) < 0x1p30f ? fmaf(mx[t][c], F[t][c], -at) : 0.0f;
+        const float by = exp2_fast(rest) * __uint_as_float((uint32_t)(127 - (int)up[t][c]) << 23);
         const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : by;
         const int64_t token = T.q0[b] + (there ? row / g : 0);
         const int head = h * g + row % g;
@@ -708,7 +711,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
             part[Part<D, NT>::kRows * D + r] = m;
             part[Part<D, NT>::kRows * (D + 1) + r] = sum * by;
           } else if (a.lse) {
-            a.lse[token * a.q_heads + head] = sum == 0.0f ? -kInf : kLn2 * (m - up[t][c] + log2f(sum));
+            a.lse[token * a.q_heads + head] = sum == 0.0f ? -kInf : kLn2 * (at - up[t][c] + log2f(sum));
           }
         }
       }

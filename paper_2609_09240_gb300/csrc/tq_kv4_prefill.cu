@@ -106,6 +106,27 @@ __device__ __forceinline__ void tmem_wait32(uint32_t *r) {
                  "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
                  "+r"(r[30]), "+r"(r[31])::"memory");
 }
+// Two floats in one register pair.
+typedef uint64_t Pair;
+__device__ __forceinline__ Pair pair_of(uint32_t lo, uint32_t hi) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ Pair twice(float v) { return pair_of(__float_as_uint(v), __float_as_uint(v)); }
+__device__ __forceinline__ void parts_of(Pair v, float *lo, float *hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(v));
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 // The warpgroup's registers per thread from here on.  512 threads are launched
 // with 128 each; what the warpgroups take is no more.
 constexpr int kSoftRegs = 168, kDecRegs = 112, kMmaRegs = 64;
@@ -404,7 +425,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
           }
         }
         if (grow) m = top;
-        const float ref = m == -kInf ? 0.0f : m * F - kUp;
         // tokens that stand for NaN in V were decoded as zeros
         {
           const uint32_t *notes = reinterpret_cast<const uint32_t *>(smem + Y::oLost + (j & 3) * G * 16);
@@ -417,21 +437,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
 #pragma unroll
               for (int gr = 0; gr < G; ++gr) lost |= (notes[4 * gr + (k >> 5)] >> (k & 31) & 1u) << gr;
         }
-        float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        // The scores meet their reference as differences (its product with F would round
+        // away what sets scores of ten digits apart), two at a time: as single operations
+        // the subtractions would take 30 us of the pass below.
+        const Pair ref = twice(m == -kInf ? 0.0f : -m), F2 = twice(F), up = twice(kUp);
+        Pair s2[2] = {twice(0.0f), twice(0.0f)};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t p[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const float p0 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k]), F, -ref));
-            const float p1 = exp2_fast(fmaf(__uint_as_float(x[c][2 * k + 1]), F, -ref));
-            s4[2 * (k & 1)] += p0;
-            s4[2 * (k & 1) + 1] += p1;
+            float p0, p1;
+            parts_of(fma2(add2(pair_of(x[c][2 * k], x[c][2 * k + 1]), ref), F2, up), &p0, &p1);
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
+            s2[k & 1] = add2(s2[k & 1], pair_of(__float_as_uint(p0), __float_as_uint(p1)));
             p[k] = pack_out<false>(p0, p1);
           }
           tmem_st16(tS + 16 * c, p);
         }
-        l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        float even, odd;
+        parts_of(add2(s2[0], s2[1]), &even, &odd);
+        l += even + odd;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();

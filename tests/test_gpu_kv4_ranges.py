@@ -107,6 +107,43 @@ def test_zero_scales_and_growing_scores(tq):
                             kw.get("scale", D ** -0.5), "fp16")
 
 
+# ------------------------------------------------------------------- scores
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L,n,heads,group", [(400, 1, 2, 4), (400, 5, 2, 4), (30000, 1, 1, 4), (400, 210, 4, 8)])
+def test_scores_of_ten_digits(tq, dtype, D, L, n, heads, group):
+    """Scores up to 2^34, exact in float32 and at least 2^24 apart or equal: a row's
+    output is the mean of the values of its best keys, which repeat.  The
+    probabilities are 0 and 1, so of test_gpu_kv4's tolerance what remains is the
+    output's rounding, P's (2^-11 a) and the sums' (2^-17 a)."""
+    import torch
+    rng = np.random.default_rng(57)
+    c, data, table, length, _ = make(tq, [L], heads, D, seed=58, poison=False)
+    kp = data[..., PAGE * D:PAGE * D + (D // 64) * PAGE * 2].view(np.uint16)
+    kp[...] = scale_bits(10) | 8
+    few = rng.integers(0, 256, (6, heads, D // 2)).astype(np.uint8)  # six different keys
+    for t in range(L):
+        for h in range(heads):
+            data[:, table[0, t // PAGE], h, t % PAGE * (D // 2):(t % PAGE + 1) * (D // 2)] = few[t * 7 % 6 if t % 5 else 0, h]
+    c.data.copy_(dev(data))
+    q = rng.choice([-16384.0, 0.0, 16384.0], (n, heads * group, D)).astype(np.float32)
+    q = dev(q).to({"fp16": torch.float16, "bf16": torch.bfloat16}[dtype])
+    out, lse = attend(tq, c, q, [0], [n], scale=1.0)
+    got, gl, qf = out.float().cpu().numpy(), lse.cpu().numpy(), q.float().cpu().numpy().astype(np.float64)
+    for h in range(heads):
+        K, V = q4.sequence(data, table, length, 0, 0, h, D)
+        for hq in range(h * group, (h + 1) * group):
+            s = qf[:, hq] @ K.T
+            for i in range(n):
+                end = L - n + i + 1
+                best = np.flatnonzero(s[i, :end] == s[i, :end].max())
+                o, a = V[best].mean(0), np.abs(V[best]).mean(0)
+                tol = np.abs(o) * 2.0 ** (-11 if dtype == "fp16" else -8) + (2.0 ** -11 + 2.0 ** -17) * a + 2.0 ** -24
+                assert np.all(np.abs(got[i, hq] - o) <= tol), (h, hq, i, got[i, hq][:4], o[:4])
+                m = s[i, :end].max()
+                assert abs(gl[i, hq] - (m + np.log(len(best)))) <= 2.0 ** -21 * abs(m) + 2.0 ** -17
+
+
 # ------------------------------------------------------------------ windows
 @pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30, 2 ** 31 - 64])
 @pytest.mark.parametrize("lengths,n,heads,group", [([2, 0, 100, 1], [9, 3, 4, 70], 2, 4), ([2, 0, 100, 1], [210, 70, 4, 99], 4, 8)])
