@@ -626,10 +626,12 @@ TQ_API tq_status tq_kv4_read(const tq_kv4_cache *c, int32_t layer, int32_t token
  * over the positions j of its sequence that the token sees: j <= its own
  * (causal != 0) and, with window > 0, j > its own - window; all of them with
  * causal = 0 (window must then be 0).  A token that sees nothing (a position
- * below 0) gets zeros and lse -inf.  Products and sums are fp32; p (in calls
- * of few query rows p times the scale of the value's group) is rounded to
- * fp16, once, for its product with the codes: as a normal number down to 2^-21
- * of the largest of its row (and group).
+ * below 0) gets zeros and lse -inf.  Queries are multiplied as fp16, a bf16
+ * token's and head's row under a power of two (exact down to 2^-27 of its
+ * largest value).  Products and sums are fp32; p (in calls of few query rows p
+ * times the scale of the value's group) is rounded to fp16, once, for its
+ * product with the codes: as a normal number down to 2^-21 of the largest of
+ * its row (and group).
  *   q: [tokens][q_heads][dim], token t's row from element t * q_stride on
  *   (a multiple of 8), 16-byte aligned; out the same with out_stride; lse:
  *   optional fp32 [tokens][q_heads], the natural logarithm of the sum;

@@ -15,7 +15,7 @@
 // the tensor cores are idle most of the time anyway, and the decoding feeds
 // registers, where mma.sync takes its operands.
 //   * fp16 queries enter as they are; bf16 ones as fp16 times a power of two per
-//     row (their largest value in 2^10 .. 2^11), which loses nothing.
+//     row (query_exponent).
 //   * P is rounded to fp16, once.  Each row and group has a power of two of its
 //     own for it, which brings the largest p_t s_t that the row has met just below
 //     2^9: a group of small values beside one of large ones, or tokens of small
@@ -150,7 +150,7 @@ constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr int kTop = 9;             // 2^kTop: where a row's and group's largest P is put
 constexpr float kFirst = -3.0e38f;  // the reference of rows that have seen nothing
 constexpr float kMost = 0x1p100f;   // of the sum, whose exponentials follow the first group's power of two
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 // A partial result: D values of each row, then the logarithms that the values
 // refer to, then the sums.  A warp leaves at most two, of the segment that its
@@ -379,11 +379,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
         }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      // 2^e brings the largest into [2^10, 2^11); rows without a finite one stay
-      int e = 0;
-      if (BF16 && top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
-      // a negative scale turns the queries' sign, none makes them zeros: F > 0
-      float by = BF16 ? __uint_as_float((uint32_t)(127 + e) << 23) : 1.0f;
+      const int e = BF16 ? query_exponent(top) : 0;
+      // a negative scale turns the queries' sign, none makes them zeros
+      float by = power_of_two(e);
       by = a.scale < 0.0f ? -by : a.scale == 0.0f ? 0.0f : by;
 #pragma unroll
       for (int gr = 0; gr < G; ++gr)
@@ -392,8 +390,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
           qf[t][gr][2 * i] = pack_f16(x[gr][i] * by, x[gr][4 + i] * by);
           qf[t][gr][2 * i + 1] = pack_f16(x[gr][8 + i] * by, x[gr][12 + i] * by);
         }
-      const float Fr =
-          a.scale == 0.0f ? 1.0f : fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-30f);
+      const float Fr = score_factor(a.scale, e);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         F[t][c] = __shfl_sync(0xffffffffu, Fr, 4 * (2 * j + c));

@@ -1,6 +1,8 @@
 // tq_kv4_attention.cuh - arguments of the attention kernels over the 4-bit K/V cache.
 #pragma once
 
+#include <limits>
+
 #include "tq_kv4.cuh"
 
 namespace tq {
@@ -28,6 +30,24 @@ cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear);
 __device__ __forceinline__ int first_seen(int pos, int window) {
   const int64_t at = (int64_t)pos - window + 1;
   return window > 0 && at > 0 ? (int)at : 0;
+}
+
+// A query row enters the tensor cores as fp16.  A bf16 row whose largest value is
+// `top` is multiplied by 2^query_exponent(top) for that, which brings its largest
+// into [2^10, 2^11) (a tiny one as far as 2^126 goes; rows without a finite one
+// stay): values down to 2^-27 of the largest keep their bits, smaller ones are
+// rounded as subnormal numbers.
+__device__ __forceinline__ int query_exponent(float top) {
+  return top < std::numeric_limits<float>::infinity() ? min(137 - (int)(__float_as_uint(top) >> 23), 126) : 0;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// What a row's scores are multiplied by in front of exp2: positive (the query
+// takes the scale's sign, or is zeros), finite, and large enough that any score
+// is beyond the exponentials' range above a reference of -3e38 (scores stay below
+// 2^40: a smaller factor would make all weights 1 as well).
+__device__ __forceinline__ float score_factor(float scale, int e) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  return scale == 0.0f ? 1.0f : fminf(fmaxf(fabsf(scale) * kLog2e * power_of_two(-e), 1e-30f), 3.4e38f);
 }
 
 // Two results in the output's type.

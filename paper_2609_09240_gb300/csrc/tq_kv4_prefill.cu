@@ -48,7 +48,7 @@ constexpr int kThreads = 16 * 32;  // four warpgroups, for their register counts
 constexpr int kDecThreads = kDecWarps * 32;
 constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr float kGrow = 8.0f, kUp = 7.0f;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 template <int D>
 struct Lay {
@@ -327,9 +327,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       {
         const uint4 *src = reinterpret_cast<const uint4 *>(a.q + token * a.q_stride + head * D);
         unsigned char *dst = smem + Y::oQ + i * Y::kTileBytes + ((r >> 3) * C) * 128 + (r & 7) * 16;
-        float up = 1.0f;
         int e = 0;
-        if (BF16) {  // a power of two brings the row's largest value into [2^10, 2^11)
+        if (BF16) {
           float top = 0.0f;
           if (there)
 #pragma unroll
@@ -340,12 +339,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
               for (int k = 0; k < 4; ++k)
                 top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xFFFF0000u))));
             }
-          if (top > 0.0f && top <= 3.0e38f) e = min(max(137 - (int)(__float_as_uint(top) >> 23), -60), 100);
-          up = __uint_as_float((uint32_t)(127 + e) << 23);
+          e = query_exponent(top);
         }
-        // a negative scale turns the queries' sign, none makes them zeros: F > 0
+        // a negative scale turns the queries' sign, none makes them zeros
+        float up = power_of_two(e);
         up = a.scale < 0.0f ? -up : a.scale == 0.0f ? 0.0f : up;
-        if (a.scale != 0.0f) F = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e) << 23), 1e-37f);
+        F = score_factor(a.scale, e);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const uint4 v = there ? __ldg(src + c) : make_uint4(0, 0, 0, 0);

@@ -154,3 +154,18 @@ def test_windows_wider_than_any_sequence(tq, window, lengths, n, heads, group):
     q = queries(np.random.default_rng(60), sum(n), heads * group, D, "fp16")
     out, lse = attend(tq, c, q, range(4), n, window=window)
     check_attention(c, data, table, length, range(4), n, heads, group, D, 0, q, out, lse, True, window, D ** -0.5, "fp16")
+
+
+# ------------------------------------------------------------------ queries
+@pytest.mark.parametrize("e", [-126, -110, 75, 90, 124])
+@pytest.mark.parametrize("L,n,heads,group", [(300, 2, 2, 4), (300, 200, 4, 8)])
+def test_bf16_queries_of_every_size(tq, e, L, n, heads, group):
+    """Queries around 2^e with a scale that brings the scores back to ordinary ones."""
+    import torch
+    D = 128
+    c, data, table, length, _ = make(tq, [L], heads, D, seed=61)
+    q = np.clip(np.random.default_rng(62).standard_normal((n, heads * group, D)), -7, 7) * 2.0 ** e
+    q = dev(q.astype(np.float32)).to(torch.bfloat16)
+    scale = float(np.float32(2.0 ** max(-e, -126) * D ** -0.5))
+    out, lse = attend(tq, c, q, [0], [n], scale=scale)
+    check_attention(c, data, table, length, [0], [n], heads, group, D, 0, q, out, lse, True, 0, scale, "bf16")
