@@ -720,8 +720,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
     if (fresh) begin_segment(u0 + i);
     fresh = false;
     if (holds >> stage & 1) {
-      holds &= ~(1u << stage);
-      if (!__all_sync(0xffffffffu, mbar_wait(&bars[stage], phase >> stage & 1))) break;
+      const bool came = __all_sync(0xffffffffu, mbar_wait(&bars[stage], phase >> stage & 1));
+      if (came) holds &= ~(1u << stage);
+      if (!came) {
+        // the first segment may not have ended: its entry then names nobody
+        if (lane == 0) joins[w].w1 = -1;
+        break;
+      }
       phase ^= 1u << stage;
       const int tok0 = (p0 + pg) * kPage;
       const bool plain = tok0 >= some_begin && tok0 + kPage <= all_end;
@@ -749,7 +754,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1)
       }
     }
   }
-  // after a wait that ran out: no copy may land in a block that is gone
+  // after a wait that ran out: no copy, the one waited for among them, may land in a
+  // block that is gone
   for (int i = 0; i < S; ++i)
     if (holds >> i & 1) mbar_wait(&bars[i], phase >> i & 1);
 

@@ -169,3 +169,31 @@ def test_bf16_queries_of_every_size(tq, e, L, n, heads, group):
     scale = float(np.float32(2.0 ** max(-e, -126) * D ** -0.5))
     out, lse = attend(tq, c, q, [0], [n], scale=scale)
     check_attention(c, data, table, length, [0], [n], heads, group, D, 0, q, out, lse, True, 0, scale, "bf16")
+
+
+# --------------------------------------------------------------------- joins
+@pytest.mark.parametrize("lengths,n", [([300], [1]), ([5000, 1, 0], [1, 1, 1]), ([20000], [2]), ([64] * 40, [1] * 40)])
+def test_every_worker_says_what_there_is_to_join(tq, lengths, n):
+    """The kernel that joins parts reads an entry of every worker: after a call on
+    scratch memory full of ones each names workers that exist, or none."""
+    import ctypes
+    import torch
+    D, heads, group = 128, 2, 4
+    c, *_ = make(tq, lengths, heads, D, seed=63)
+    T, L = sum(n), tq.lib()
+    q = torch.randn((T, heads * group, D), device="cuda").half()
+    out, slots, indptr = torch.empty_like(q), i32(range(len(n))), i32(np.concatenate([[0], np.cumsum(n)]))
+    nbytes = L.tq_kv4_attention_workspace_bytes(c._ref, len(n), T, max(n), heads * group)
+    ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+    p = lambda t: ctypes.c_void_p(t.data_ptr())
+    assert L.tq_kv4_attention(c._ref, 0, len(n), p(slots), p(indptr), T, max(n), heads * group, 0, p(q), heads * group * D,
+                              D ** -0.5, 1, 0, p(out), heads * group * D, None, p(ws), nbytes, p(c.status), None) == 0
+    torch.cuda.synchronize()
+    c.check()
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    workers = sms * 12 if max(n) * group <= 8 else sms * 8  # warps of the chip; an entry is 48 bytes, its second word the last worker
+    entries = ws[:workers * 48].view(torch.int32).view(workers, 12).cpu().numpy()
+    some = entries[:, 1] >= 0
+    assert np.all(entries[:, 1] >= -1) and np.all(entries[:, 1] < workers)
+    assert np.all(entries[some, 0] >= 0) and np.all(entries[some, 0] < entries[some, 1])
+    assert np.all(entries[some, 7] < T) and np.all(entries[some, 8] < heads)
