@@ -528,6 +528,8 @@ TQ_API tq_status tq_linear_static(int32_t M, int32_t N, int32_t K, const tq_weig
  * (table and data may hold anything).  Table entries beyond a sequence's
  * pages are not read.  All state is device memory and every call is
  * asynchronous: a step can be captured in a graph and grows no host state.
+ * Calls that may overlap in time need workspaces of their own, a captured one
+ * whenever its graph is replayed beside other work.
  *
  * Errors in device data (a slot or page out of range, a list that names a
  * slot twice, too few free pages) are OR-ed into *d_status; nothing out of

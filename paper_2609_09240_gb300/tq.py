@@ -813,7 +813,9 @@ def _raw_stream(stream):
 
 class Kv4Cache:
     """A 4-bit K/V cache (tq_kv4_cache): device tensors, a status word that the
-    calls OR data errors into, and their scratch memory (one per stream).
+    calls OR data errors into, and their scratch memory (one block per stream for
+    eager calls; calls captured in a graph have their own, and ws= gives a call the
+    caller's).
 
     data uint8 [layers][pages][heads][block], table int32 [slots][max_pages],
     length int32 [slots], refs int32 [pages]."""
@@ -843,10 +845,16 @@ class Kv4Cache:
         return cls(torch.empty((layers, pages, heads, block), dtype=torch.uint8, device=device),
                    torch.full((slots, max_pages), -1, **i32), torch.zeros(slots, **i32), torch.zeros(pages, **i32), dim)
 
-    def _scratch(self, stream, fn, *args):
-        """The stream's scratch memory, at least as large as `fn`(cache, *args)
-        says.  One that was outgrown is kept (work in flight may use it); sizes
-        double, so all of them together are no more than twice the largest."""
+    def _scratch(self, ws, stream, fn, *args):
+        """Scratch memory for a call: the caller's `ws`, or else at least as much as
+        `fn`(cache, *args) says.  Eager calls on a stream share one block; one that
+        was outgrown is kept (work in flight may use it); sizes double, so all of
+        them together are no more than twice the largest.  While the stream is
+        captured every call has a block of its own from the graph's memory: the
+        graph may be replayed on any stream, beside other graphs and eager calls."""
+        if ws is not None:
+            _want(ws, "ws", torch.uint8)
+            return ws
         key = (fn, args)
         n = self._sizes.get(key)
         if n is None:
@@ -856,13 +864,15 @@ class Kv4Cache:
             if len(self._sizes) >= 4096:
                 self._sizes.clear()
             self._sizes[key] = n
+        if torch.cuda.is_current_stream_capturing():
+            return workspace(n, self.device)
         ws = self._ws.get(stream)
         if ws is None or ws.numel() < n:
             if ws is not None:
                 self._outgrown.append(ws)
                 n = max(n, 2 * ws.numel())
-            ws = self._ws[stream] = workspace(n, self.data.device)
-        return ws.data_ptr(), ws.numel()
+            ws = self._ws[stream] = workspace(n, self.device)
+        return ws
 
     def check(self):
         """Raise on data errors that earlier calls reported (synchronizes; clears them)."""
@@ -872,7 +882,7 @@ class Kv4Cache:
             raise TQError(-4, f"4-bit cache: data status {st:#x}")
 
 
-def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, where=None, stream=None):
+def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, where=None, stream=None, ws=None):
     """Room for counts[i] new tokens at the end of sequences slots[i] (int32
     device lists; tokens: their sum).  Returns (indptr [count + 1], where
     [tokens]), the token ranges for tq_kv4_attention and the places for
@@ -883,12 +893,12 @@ def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, wher
     if where is None:
         where = torch.empty(tokens, dtype=torch.int32, device=slots.device)
     st = _raw_stream(stream)
-    ws, nws = cache._scratch(st, "tq_kv4_extend_workspace_bytes", n, tokens)
+    ws = cache._scratch(ws, st, "tq_kv4_extend_workspace_bytes", n, tokens)
     i32 = torch.int32
     _check((_lib or lib()).tq_kv4_extend(
         cache._ref, n, _want(slots, "slots", i32, (n,)), _want(counts, "counts", i32, (n,)), tokens,
-        _want(indptr, "indptr", i32, (n + 1,)), _want(where, "where", i32, (tokens,)), ws, nws, cache._status, st),
-        "tq_kv4_extend")
+        _want(indptr, "indptr", i32, (n + 1,)), _want(where, "where", i32, (tokens,)), ws.data_ptr(), ws.numel(),
+        cache._status, st), "tq_kv4_extend")
     return indptr, where
 
 
@@ -907,7 +917,7 @@ def tq_kv4_free(cache: Kv4Cache, slots, keep=None, stream=None):
                              _raw_stream(stream)), "tq_kv4_free")
 
 
-def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, live=None, stream=None):
+def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, live=None, stream=None, ws=None):
     """The pages in use moved to the front of the pool; table and refs change
     in place unless table_out / refs_out are given.  Returns (remap [pages],
     live [1])."""
@@ -917,11 +927,11 @@ def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, l
     remap = torch.empty(cache.pages, **i32) if remap is None else remap
     live = torch.empty(1, **i32) if live is None else live
     st = _raw_stream(stream)
-    ws, nws = cache._scratch(st, "tq_kv4_compact_workspace_bytes")
+    ws = cache._scratch(ws, st, "tq_kv4_compact_workspace_bytes")
     _check((_lib or lib()).tq_kv4_compact(cache._ref, _want(table_out, "table_out", torch.int32, cache.table.shape),
                                 _want(refs_out, "refs_out", torch.int32, cache.refs.shape),
                                 _want(remap, "remap", torch.int32, (cache.pages,)),
-                                _want(live, "live", torch.int32, (1,)), ws, nws, cache._status, st),
+                                _want(live, "live", torch.int32, (1,)), ws.data_ptr(), ws.numel(), cache._status, st),
            "tq_kv4_compact")
     return remap, live
 
@@ -970,7 +980,7 @@ def tq_kv4_read(cache: Kv4Cache, layer: int, where, dtype=torch.float16, k=None,
 
 
 def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, scale=None, causal=True, window=0,
-                     out=None, lse=None, stream=None):
+                     out=None, lse=None, stream=None, ws=None):
     """Attention of q [tokens][q_heads][dim] (fp16 or bf16) over one layer of
     the cache; sequence slots[b] has the queries indptr[b] .. indptr[b + 1] - 1,
     its last tokens.  max_q: the most queries of a sequence, if known (1 in a
@@ -989,12 +999,12 @@ def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, 
     n = slots.shape[0]
     max_q = T if max_q is None or max_q > T else int(max_q)
     st = _raw_stream(stream)
-    ws, nws = cache._scratch(st, "tq_kv4_attention_workspace_bytes", n, T, max_q, Hq)
+    ws = cache._scratch(ws, st, "tq_kv4_attention_workspace_bytes", n, T, max_q, Hq)
     lp = None if lse is None else _want(lse, "lse", torch.float32, (T, Hq))
     _check((_lib or lib()).tq_kv4_attention(
         cache._ref, layer, n, _want(slots, "slots", torch.int32, (n,)), _want(indptr, "indptr", torch.int32, (n + 1,)),
         T, max_q, Hq, _KV_DTYPE[dtype], qp, qs, dim ** -0.5 if scale is None else scale, causal, window, op, os_, lp,
-        ws, nws, cache._status, st), "tq_kv4_attention")
+        ws.data_ptr(), ws.numel(), cache._status, st), "tq_kv4_attention")
     return out
 
 
