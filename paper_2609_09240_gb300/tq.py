@@ -875,7 +875,9 @@ class Kv4Cache:
         return ws
 
     def check(self):
-        """Raise on data errors that earlier calls reported (synchronizes; clears them)."""
+        """Raise on data errors that earlier calls reported, on any stream (waits for the
+        device; clears them)."""
+        torch.cuda.synchronize(self.device)
         st = int(self.status.item())
         if st:
             self.status.zero_()
@@ -887,12 +889,15 @@ def tq_kv4_extend(cache: Kv4Cache, slots, counts, tokens: int, indptr=None, wher
     device lists; tokens: their sum).  Returns (indptr [count + 1], where
     [tokens]), the token ranges for tq_kv4_attention and the places for
     tq_kv4_append."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return tq_kv4_extend(cache, slots, counts, tokens, indptr, where, ws=ws)
     n = slots.shape[0]
     if indptr is None:
         indptr = torch.empty(n + 1, dtype=torch.int32, device=slots.device)
     if where is None:
         where = torch.empty(tokens, dtype=torch.int32, device=slots.device)
-    st = _raw_stream(stream)
+    st = _raw_stream(None)
     ws = cache._scratch(ws, st, "tq_kv4_extend_workspace_bytes", n, tokens)
     i32 = torch.int32
     _check((_lib or lib()).tq_kv4_extend(
@@ -921,12 +926,15 @@ def tq_kv4_compact(cache: Kv4Cache, table_out=None, refs_out=None, remap=None, l
     """The pages in use moved to the front of the pool; table and refs change
     in place unless table_out / refs_out are given.  Returns (remap [pages],
     live [1])."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return tq_kv4_compact(cache, table_out, refs_out, remap, live, ws=ws)
     i32 = dict(dtype=torch.int32, device=cache.data.device)
     table_out = cache.table if table_out is None else table_out
     refs_out = cache.refs if refs_out is None else refs_out
     remap = torch.empty(cache.pages, **i32) if remap is None else remap
     live = torch.empty(1, **i32) if live is None else live
-    st = _raw_stream(stream)
+    st = _raw_stream(None)
     ws = cache._scratch(ws, st, "tq_kv4_compact_workspace_bytes")
     _check((_lib or lib()).tq_kv4_compact(cache._ref, _want(table_out, "table_out", torch.int32, cache.table.shape),
                                 _want(refs_out, "refs_out", torch.int32, cache.refs.shape),
@@ -959,6 +967,9 @@ def tq_kv4_append(k, v, cache: Kv4Cache, layer: int, where, stream=None):
 
 def tq_kv4_read(cache: Kv4Cache, layer: int, where, dtype=torch.float16, k=None, v=None, stream=None):
     """The keys and values held at the places where[]: two [tokens][heads][dim] tensors."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return tq_kv4_read(cache, layer, where, dtype, k, v)
     if dtype not in _KV_DTYPE:
         raise ValueError(f"expected fp16 or bf16, got {dtype}")
     T = where.shape[0]
@@ -975,7 +986,7 @@ def tq_kv4_read(cache: Kv4Cache, layer: int, where, dtype=torch.float16, k=None,
     else:
         vp = _want(v, "v", dtype, shape)
     _check((_lib or lib()).tq_kv4_read(cache._ref, layer, T, _KV_DTYPE[dtype], wp, kp, vp, cache._status,
-                                       _raw_stream(stream)), "tq_kv4_read")
+                                       _raw_stream(None)), "tq_kv4_read")
     return k, v
 
 
@@ -986,6 +997,9 @@ def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, 
     its last tokens.  max_q: the most queries of a sequence, if known (1 in a
     decode step).  scale: 1 / sqrt(dim) if None.  lse: optional fp32
     [tokens][q_heads] output.  Returns out."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return tq_kv4_attention(q, cache, layer, slots, indptr, max_q, scale, causal, window, out, lse, ws=ws)
     qp, qs = _rows(q, "q", None, cache.dim)
     T, Hq, dim = q.shape
     dtype = q.dtype
@@ -998,7 +1012,7 @@ def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, 
             raise ValueError("out and q differ in tokens or type")
     n = slots.shape[0]
     max_q = T if max_q is None or max_q > T else int(max_q)
-    st = _raw_stream(stream)
+    st = _raw_stream(None)
     ws = cache._scratch(ws, st, "tq_kv4_attention_workspace_bytes", n, T, max_q, Hq)
     lp = None if lse is None else _want(lse, "lse", torch.float32, (T, Hq))
     _check((_lib or lib()).tq_kv4_attention(
@@ -1044,37 +1058,49 @@ def _w4_made(call, where, dev, check):
 def pack_w4(codes, scale, minimum, stream=None, check=True) -> W4Weight:
     """uint8 codes [N][K] (0 .. 15), fp16 scale and minimum [N][K / 128] ->
     W4Weight.  check reads the data status back (one synchronization)."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return pack_w4(codes, scale, minimum, check=check)
     N, K = codes.shape
     w = W4Weight._new(N, K, codes.device)
     g = (N, K // TQ_GROUP)
     cp, sp, mp = (_want(codes, "codes", torch.uint8), _want(scale, "scale", torch.float16, g),
                   _want(minimum, "minimum", torch.float16, g))
-    _w4_made(lambda st: lib().tq_w4_pack(N, K, cp, sp, mp, _p(w.tiles), st, _raw_stream(stream)), "tq_w4_pack",
+    _w4_made(lambda st: lib().tq_w4_pack(N, K, cp, sp, mp, _p(w.tiles), st, _raw_stream(None)), "tq_w4_pack",
              codes.device, check)
     return w
 
 
 def quantize_w4(W, stream=None, check=True) -> W4Weight:
     """Round-to-nearest 4-bit weights of fp16 W [N][K] on the device."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return quantize_w4(W, check=check)
     N, K = W.shape
     w = W4Weight._new(N, K, W.device)
     wp = _want(W, "W", torch.float16)
-    _w4_made(lambda st: lib().tq_w4_quantize(N, K, wp, _p(w.tiles), st, _raw_stream(stream)), "tq_w4_quantize", W.device,
+    _w4_made(lambda st: lib().tq_w4_quantize(N, K, wp, _p(w.tiles), st, _raw_stream(None)), "tq_w4_quantize", W.device,
              check)
     return w
 
 
 def tq_w4_dequantize(w: W4Weight, out=None, stream=None):
     """W as dense fp16 [N][K] on the device."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return tq_w4_dequantize(w, out)
     if out is None:
         out = torch.empty((w.N, w.K), dtype=torch.float16, device=w.tiles.device)
-    _check((_lib or lib()).tq_w4_dequantize(w.N, w.K, w._ref, _want(out, "out", torch.float16, (w.N, w.K)), _raw_stream(stream)),
+    _check((_lib or lib()).tq_w4_dequantize(w.N, w.K, w._ref, _want(out, "out", torch.float16, (w.N, w.K)), _raw_stream(None)),
            "tq_w4_dequantize")
     return out
 
 
 def tq_w4_linear(x, w: W4Weight, y=None, ws=None, stream=None, f32=False):
     """y = x W^T for 4-bit weights; x fp16 [M][K], y fp16 [M][N] (fp32 with f32=True)."""
+    if stream is not None:  # what the call allocates and waits for is the stream's
+        with torch.cuda.stream(stream):
+            return tq_w4_linear(x, w, y, ws, f32=f32)
     M = x.shape[0]
     dt = torch.float32 if f32 else torch.float16
     xp = _want(x, "x", torch.float16, (M, w.K))
@@ -1086,5 +1112,5 @@ def tq_w4_linear(x, w: W4Weight, y=None, ws=None, stream=None, f32=False):
     wsp, nws = (w._scratch, 256) if ws is None else (_want(ws, "ws", torch.uint8), ws.numel())
     L = _lib or lib()
     fn = L.tq_w4_linear_f32out if f32 else L.tq_w4_linear
-    _check(fn(M, w.N, w.K, w._ref, xp, yp, wsp, nws, _raw_stream(stream)), "tq_w4_linear")
+    _check(fn(M, w.N, w.K, w._ref, xp, yp, wsp, nws, _raw_stream(None)), "tq_w4_linear")
     return y

@@ -102,3 +102,61 @@ def test_callers_workspace(tq):
     with pytest.raises(tq.TQError):
         tq.tq_kv4_compact(c, ws=torch.empty(0, dtype=torch.uint8, device="cuda"))
     c.check()
+
+
+# ------------------------------------------------------------------ streams
+def stream_of(t):
+    """The stream whose memory a tensor lives in."""
+    import torch
+    p = t.data_ptr()
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= p < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not the allocator's memory")
+
+
+def test_memory_comes_from_the_stream_that_uses_it(tq):
+    """Memory freed on the current stream may still be in use there: what a call on
+    another stream allocates has to be that stream's."""
+    import torch
+    c, *_ = make(tq, [300, 70], 2, 128, seed=3)
+    q = torch.randn((2, 8, 128), device="cuda").half()
+    W, x = torch.randn((64, 256), device="cuda").half(), torch.randn((2, 256), device="cuda").half()
+    codes, s, m = torch.ones((64, 256), dtype=torch.uint8, device="cuda"), W[:, :2].contiguous(), W[:, 2:4].contiguous()
+    slots, ip, one = i32([0, 1]), i32([0, 1, 2]), i32([1, 1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = tq.tq_kv4_attention(q, c, 0, slots, ip, max_q=1, stream=side)
+    indptr, where = tq.tq_kv4_extend(c, slots, one, 2, stream=side)
+    k, v = tq.tq_kv4_read(c, 0, where, stream=side)
+    remap, live = tq.tq_kv4_compact(c, stream=side)
+    a, b = tq.quantize_w4(W, stream=side), tq.pack_w4(codes, s, m, stream=side)
+    y, D = tq.tq_w4_linear(x, a, stream=side), tq.tq_w4_dequantize(a, stream=side)
+    torch.cuda.synchronize()
+    c.check()
+    for t in (out, indptr, where, k, v, remap, live, a.tiles, b.tiles, y, D, *c._ws.values()):
+        assert stream_of(t) == side.cuda_stream
+    assert stream_of(q) == torch.cuda.current_stream().cuda_stream
+
+
+def test_errors_reported_on_another_stream_are_seen(tq):
+    """The reports of work that is still under way on another stream."""
+    import torch
+    c, *_ = make(tq, [100], 2, 128, seed=4)
+    k = torch.ones((1, 2, 128), device="cuda").half()
+    W = torch.full((16, 128), float("nan"), device="cuda").half()
+    codes, s = torch.full((16, 128), 16, dtype=torch.uint8, device="cuda"), torch.ones((16, 1), device="cuda").half()
+    beyond = i32([c.pages * 64])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for call in (lambda: tq.quantize_w4(W, stream=side), lambda: tq.pack_w4(codes, s, s, stream=side)):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)  # about 50 ms
+        with pytest.raises(tq.TQError):
+            call()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    tq.tq_kv4_append(k, k, c, 0, beyond, stream=side)
+    with pytest.raises(tq.TQError):
+        c.check()
+    c.check()
