@@ -63,10 +63,9 @@ struct SeqTable {
   int32_t L[kMaxSeqs], n[kMaxSeqs], q0[kMaxSeqs], slot[kMaxSeqs];
 };
 
-// Pages [p0, p1) that any query of the sequence sees.
+// Pages that any query of the sequence sees.
 __device__ __forceinline__ void seq_pages(const AttnArgs &a, int L, int n, int *p0, int *np) {
-  *p0 = first_seen(L - n, a.window) / kPage;
-  *np = (L + kPage - 1) / kPage - *p0;
+  *np = pages_seen(L, n, a.window, p0);
 }
 
 // Fills the table; every thread of the block calls it.  part: scratch.
@@ -74,27 +73,34 @@ template <int WARPS>
 __device__ __forceinline__ void load_seqs(const AttnArgs &a, int rows_per_tile, SeqTable &T, int64_t *part) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = a.q_heads / a.c.heads;
+  uint64_t all_work = 0;
+  if (a.many) {
+    for (int b = tid; b < a.all_count; b += WARPS * 32)
+      all_work += work_of_many(a, sequence_of(a, a.all_slots, a.all_indptr, b));
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) all_work += __shfl_xor_sync(0xffffffffu, all_work, d);
+    if (lane == 0) part[warp] = (int64_t)all_work;
+    __syncthreads();
+    all_work = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) all_work += (uint64_t)part[w];
+    __syncthreads();
+  }
   int64_t carry = 0;
   for (int base = 0; base < a.count; base += WARPS * 32) {
     const int b = base + tid;
     int64_t u = 0;
     if (b < a.count) {
-      const int slot = a.slots[b], q0 = a.indptr[b], n = a.indptr[b + 1] - q0;
-      int L = 0;
-      bool bad = slot < 0 || slot >= a.c.slots || q0 < 0 || n < 0 || n > a.tokens - q0;
-      if (!bad) {
-        L = a.c.length[slot];
-        bad = L != clamp_length(a.c, L);
-      }
-      if (bad && blockIdx.x == 0) report(a.d_status, TQ_DATA_BAD_SLOT);
-      T.slot[b] = slot;
-      T.q0[b] = q0;
-      T.L[b] = L;
-      T.n[b] = bad ? 0 : n;
-      if (!bad && n > 0 && (int64_t)n * g < a.many_rows) {
+      const Sequence s = sequence_of(a, a.slots, a.indptr, b);
+      if (!s.good && blockIdx.x == 0) report(a.d_status, TQ_DATA_BAD_SLOT);
+      T.slot[b] = s.slot;
+      T.q0[b] = s.q0;
+      T.L[b] = s.L;
+      T.n[b] = s.good ? s.n : 0;
+      if (s.good && s.n > 0 && !(a.many && goes_to_tiles(a, s, all_work))) {
         int p0, np;
-        seq_pages(a, L, n, &p0, &np);
-        const int tiles = (int)(((int64_t)n * g + rows_per_tile - 1) / rows_per_tile);
+        seq_pages(a, s.L, s.n, &p0, &np);
+        const int tiles = (int)(((int64_t)s.n * g + rows_per_tile - 1) / rows_per_tile);
         // a sequence without pages keeps one unit per tile and head: its rows are zeros
         u = (int64_t)max(np, 1) * tiles * a.c.heads;
       }
@@ -819,20 +825,6 @@ inline size_t split_ws_bytes(int D, int NT) {
   const int warps = NT == 1 ? Shape<128, 1>::kWarps : Shape<128, 2>::kWarps;
   return (size_t)sm_count() * warps * (sizeof(Join) + 2 * (8 * NT) * (D + 2) * 4);
 }
-// Which kernel a sequence's rows go to.  The kernel for many rows takes 256 of
-// them at a time, 2.3 us per 128 keys whatever their number, and a block does a
-// task to its end; the kernel for few rows spreads a chip-wide 2.9 ns per 64 keys,
-// head and 16 rows evenly.  They meet at 6000 rows (of all heads and sequences)
-// per wave of blocks: for 16 sequences with 8 K/V heads 48 rows each take 65 us in
-// the one and 58 in the other, 32 rows 48 and 57; for one sequence with 8 heads of
-// 6000 keys 256 rows take 49 and 106.  Within a call, sequences with fewer than 48
-// rows per head (a decode step among prompts) stay with the kernel for few.
-constexpr int kManyRows = 48, kManyAtOnce = 6000;
-inline bool many_rows(int64_t tokens, int max_q, int q_heads, int heads) {
-  const int64_t rows = tokens * q_heads, sms = sm_count();
-  const int64_t waves = std::max<int64_t>(1, (rows + 256 * sms - 1) / (256 * sms));
-  return (int64_t)max_q * (q_heads / heads) >= kManyRows && rows >= kManyAtOnce * waves;
-}
 inline int split_tiles(int max_q, int group) { return (int64_t)max_q * group <= 8 ? 1 : 2; }
 
 template <int D, int NT, bool BF16>
@@ -899,10 +891,10 @@ tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t count, 
   if (workspace_bytes < tq_kv4_attention_workspace_bytes(c, count, tokens, max_q, q_heads)) return TQ_ERR_SHAPE;
   if (tokens == 0) return TQ_OK;
   const int g = q_heads / c->heads;
-  const bool many = many_rows(tokens, max_q, q_heads, c->heads), bf16 = dtype == TQ_BF16;
+  const bool many = call_of_many(tokens, max_q, q_heads, c->heads, c->dim), bf16 = dtype == TQ_BF16;
   const AttnArgs a = {*c,  layer,    count,      tokens, q_heads,  causal != 0, window,
                       slots, indptr, q,          out,    lse,      q_stride,    out_stride,
-                      scale, d_status, many ? kManyRows : 0x7fffffff};
+                      scale, d_status, many,       count,  slots,    indptr};
   cudaStream_t st = (cudaStream_t)stream;
   if (many) {
     const cudaError_t e = launch_attn_prefill(a, bf16, st);

@@ -4,6 +4,7 @@
 #include <limits>
 
 #include "tq_kv4.cuh"
+#include "tq_kv4_rule.cuh"
 
 namespace tq {
 namespace kv4 {
@@ -18,18 +19,39 @@ struct AttnArgs {
   int64_t q_stride, out_stride;
   float scale;
   uint32_t *d_status;
-  // sequences with this many query rows per K/V head or more are the kernel's
-  // for many rows (tq_kv4_prefill.cu)
-  int32_t many_rows;
+  // the whole call's lists, where some of its sequences may be the kernel's for
+  // many rows (tq_kv4_rule.cuh); none of them without `many`
+  int32_t many, all_count;
+  const int32_t *all_slots, *all_indptr;
 };
 cudaError_t launch_attn_prefill(const AttnArgs &a, bool bf16, cudaStream_t st);
 cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear);
 
-// The first position that a query at `pos` (below 0: before the sequence) sees;
-// a window may be as wide as its type.
-__device__ __forceinline__ int first_seen(int pos, int window) {
-  const int64_t at = (int64_t)pos - window + 1;
-  return window > 0 && at > 0 ? (int)at : 0;
+// Entry b of the lists; good: its slot, range and length are.
+struct Sequence {
+  int slot, q0, n, L;
+  bool good;
+};
+__device__ __forceinline__ Sequence sequence_of(const AttnArgs &a, const int32_t *slots, const int32_t *indptr, int b) {
+  Sequence s;
+  s.slot = slots[b];
+  s.q0 = indptr[b];
+  s.n = indptr[b + 1] - s.q0;
+  s.L = 0;
+  s.good = s.slot >= 0 && s.slot < a.c.slots && s.q0 >= 0 && s.n >= 0 && s.n <= a.tokens - s.q0;
+  if (s.good) {
+    s.L = a.c.length[s.slot];
+    s.good = s.L == clamp_length(a.c, s.L);
+  }
+  return s;
+}
+__device__ __forceinline__ uint64_t work_of_many(const AttnArgs &a, const Sequence &s) {
+  int p0;
+  return s.good ? work_of_many(s.n, a.q_heads, a.c.heads, pages_seen(s.L, s.n, a.window, &p0)) : 0;
+}
+__device__ __forceinline__ bool goes_to_tiles(const AttnArgs &a, const Sequence &s, uint64_t all) {
+  int p0;
+  return s.good && goes_to_tiles(s.n, a.q_heads, a.c.heads, a.c.dim, pages_seen(s.L, s.n, a.window, &p0), all);
 }
 
 // A query row enters the tensor cores as fp16.  A bf16 row whose largest value is

@@ -187,6 +187,61 @@ struct Task {
   int t0, tiles[2];          // first token; K/V tiles of each row tile
 };
 
+__device__ __forceinline__ int row_tiles(const AttnArgs &a, const Sequence &q, uint64_t all) {
+  return goes_to_tiles(a, q, all) ? (int)(((int64_t)q.n * (a.q_heads / a.c.heads) + 2 * kTile - 1) / (2 * kTile)) : 0;
+}
+// The sequence and row tile with `want` tiles before it, sequence by sequence from
+// each one's end; b = -1 where there are fewer.  Valid in thread 0; every thread of
+// the block calls it.  Its scratch memory is the tiles' to be (of its own, it would
+// take the block over 196 KB and half of the L1 cache away: 4 us of 355).
+struct Found {
+  int b, tile;
+};
+struct FindScratch {
+  uint64_t work[kThreads / 32];
+  int tiles[kThreads], found;
+};
+__device__ __forceinline__ Found find_in_order(const AttnArgs &a, int64_t want, FindScratch &sm) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  Found f = {-1, 0};
+  uint64_t all = 0;
+  for (int b = tid; b < a.count; b += kThreads) all += work_of_many(a, sequence_of(a, a.slots, a.indptr, b));
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+  if (lane == 0) sm.work[warp] = all;
+  if (tid == 0) sm.found = -1;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) all += sm.work[w];
+  for (int base = 0; base < a.count && sm.found < 0; base += kThreads) {
+    const int b = base + tid;
+    sm.tiles[tid] = b < a.count ? row_tiles(a, sequence_of(a, a.slots, a.indptr, b), all) : 0;
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll 1
+      for (int k = 0; k < kThreads && f.b < 0; k += 32) {
+        int x = sm.tiles[k + lane];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, d);
+          if (lane >= d) x += y;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, want < x);
+        if (hit) {
+          f.b = base + k + __ffs(hit) - 1;
+          f.tile = __shfl_sync(0xffffffffu, x, __ffs(hit) - 1) - 1 - (int)want;
+        } else {
+          want -= __shfl_sync(0xffffffffu, x, 31);
+        }
+      }
+      if (lane == 0) sm.found = f.b;
+    }
+    __syncthreads();
+  }
+  return f;
+}
+
 // One block: 256 rows.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArgs a) {
@@ -218,27 +273,33 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
   // row tiles with the most keys come first: with up to 32 sequences over all of
   // them (the last wave of blocks is then the short ones: three prompts' pass
   // takes 6 % less), else sequence by sequence.
-  if (warp == 0) {
-    const int64_t want = blockIdx.x / a.c.heads;
-    int found = -1, tile = 0;
-    // of sequence b: its row tiles, and what precedes its first query
-    auto sequence = [&](int b, int *n, int *q0, int *before) {
-      *n = *q0 = *before = 0;
-      if (b >= a.count) return 0;
-      const int slot = a.slots[b];
-      *q0 = a.indptr[b];
-      *n = a.indptr[b + 1] - *q0;
-      // bad ones are reported by the kernel for few rows, small ones are its own
-      if (*q0 < 0 || *n < 0 || *n > a.tokens - *q0 || slot < 0 || slot >= a.c.slots || (int64_t)*n * g < a.many_rows)
-        return 0;
-      const int L = a.c.length[slot];
-      if (L != clamp_length(a.c, L)) return 0;
-      *before = L - *n;
-      return (int)(((int64_t)*n * g + 2 * kTile - 1) / (2 * kTile));
-    };
-    int n, q0, before;
-    if (a.count <= 32) {
-      const int tiles = sequence(lane, &n, &q0, &before);
+  const int64_t want = blockIdx.x / a.c.heads;
+  // tile `t` of sequence b, or nothing to do
+  auto take = [&](int b, const Sequence &q, int t) {
+    const int before = q.L - q.n;
+    T.b = b;
+    T.h = blockIdx.x % a.c.heads;
+    T.slot = q.slot;
+    T.L = q.L;
+    T.n = q.n;
+    T.q0 = q.q0;
+    T.row0 = t * 2 * kTile;
+    T.rows = min(q.n * g - T.row0, 2 * kTile);
+    const int first = before + T.row0 / g;  // position of the first row
+    T.t0 = first_seen(first, a.window) / kPage * kPage;
+    for (int i = 0; i < 2; ++i) {
+      const int r = min(T.rows, (i + 1) * kTile) - 1;  // the row tile's last row
+      const int end = r < i * kTile ? 0 : a.causal ? before + (T.row0 + r) / g + 1 : T.L;
+      T.tiles[i] = end > T.t0 ? (end - T.t0 + kTile - 1) / kTile : 0;
+    }
+  };
+  if (a.count <= 32) {
+    if (warp == 0) {
+      const Sequence q = lane < a.count ? sequence_of(a, a.slots, a.indptr, lane) : Sequence{0, 0, 0, 0, false};
+      uint64_t all = work_of_many(a, q);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+      const int tiles = row_tiles(a, q, all), before = q.L - q.n;
       // how many of the lane's tiles have at least v tiles of keys (by their last row)
       auto at_least = [&](int v) {
         const int64_t y = (int64_t)v * kTile - before;  // its last query is at least the y-th
@@ -260,49 +321,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       }
       const int64_t rest = want - __reduce_add_sync(0xffffffffu, more);
       const uint32_t hit = __ballot_sync(0xffffffffu, rest >= x - here && rest < x);
-      if (hit) {
-        found = __ffs(hit) - 1;
-        tile = __shfl_sync(0xffffffffu, tiles - more - 1 - (int)(rest - (x - here)), found);
-      }
-    } else {
-      int64_t rest = want;
-      for (int base = 0; base < a.count && found < 0; base += 32) {
-        const int tiles = sequence(base + lane, &n, &q0, &before);
-        int x = tiles;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, x, d);
-          if (lane >= d) x += y;
-        }
-        const uint32_t hit = __ballot_sync(0xffffffffu, rest < x);
-        if (hit) {
-          found = base + __ffs(hit) - 1;
-          tile = __shfl_sync(0xffffffffu, x, found - base) - 1 - (int)rest;  // from the sequence's end
-        } else {
-          rest -= __shfl_sync(0xffffffffu, x, 31);
-        }
-      }
+      if (hit >> lane & 1) take(lane, q, tiles - more - 1 - (int)(rest - (x - here)));
+      if (!hit && lane == 0) T.b = -1;
     }
-    if (lane == 0) {
-      T.b = found;
-      if (found >= 0) {
-        sequence(found, &n, &q0, &before);
-        T.h = blockIdx.x % a.c.heads;
-        T.slot = a.slots[found];
-        T.L = before + n;
-        T.n = n;
-        T.q0 = q0;
-        T.row0 = tile * 2 * kTile;
-        T.rows = min(n * g - T.row0, 2 * kTile);
-        const int first = before + T.row0 / g;  // position of the first row
-        T.t0 = first_seen(first, a.window) / kPage * kPage;
-        for (int i = 0; i < 2; ++i) {
-          const int r = min(T.rows, (i + 1) * kTile) - 1;  // the row tile's last row
-          const int end = r < i * kTile ? 0 : a.causal ? before + (T.row0 + r) / g + 1 : T.L;
-          T.tiles[i] = end > T.t0 ? (end - T.t0 + kTile - 1) / kTile : 0;
-        }
-      }
-    }
+  } else {
+    const Found at = find_in_order(a, want, *reinterpret_cast<FindScratch *>(smem + Y::oK));
+    if (tid == 0 && at.b >= 0) take(at.b, sequence_of(a, a.slots, a.indptr, at.b), at.tile);
+    if (tid == 0 && at.b < 0) T.b = -1;
   }
   if (warp == kMmaWarp) tmem_alloc(&bars->tmem, 512);
   tc_fence_before();
@@ -658,10 +683,11 @@ TQ_STATUS_ACCESSOR(read_status_impl)
 
 cudaError_t read_status_kv4_prefill(uint32_t *out, bool clear) { return pf::read_status_impl(out, clear); }
 
-// The sequences with at least a.many_rows query rows per K/V head.
+// The sequences that go to the tiles (tq_kv4_rule.cuh).
 cudaError_t launch_attn_prefill(const AttnArgs &a, bool bf16, cudaStream_t st) {
   const int g = a.q_heads / a.c.heads;
-  const int64_t blocks = ((int64_t)a.tokens * g / (2 * pf::kTile) + a.count) * a.c.heads;
+  static_assert(2 * pf::kTile == kTileRows, "rows of a task");
+  const int64_t blocks = most_row_tiles(a.tokens, g, a.count) * a.c.heads;
   if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
   auto go = [&](auto kern, int smem) {
     return launch_big_smem(kern, (int)blocks, pf::kThreads, smem, st, a);

@@ -994,8 +994,9 @@ def tq_kv4_attention(q, cache: Kv4Cache, layer: int, slots, indptr, max_q=None, 
                      out=None, lse=None, stream=None, ws=None):
     """Attention of q [tokens][q_heads][dim] (fp16 or bf16) over one layer of
     the cache; sequence slots[b] has the queries indptr[b] .. indptr[b + 1] - 1,
-    its last tokens.  max_q: the most queries of a sequence, if known (1 in a
-    decode step).  scale: 1 / sqrt(dim) if None.  lse: optional fp32
+    its last tokens.  max_q: the most queries of a sequence (1 in a decode step);
+    without it one sequence could have all tokens, which costs a large batch of
+    single tokens half as much again.  scale: 1 / sqrt(dim) if None.  lse: optional fp32
     [tokens][q_heads] output.  Returns out."""
     if stream is not None:  # what the call allocates and waits for is the stream's
         with torch.cuda.stream(stream):
