@@ -45,8 +45,8 @@ inline tq_status check_cache(const tq_kv4_cache *c) {
   return TQ_OK;
 }
 inline tq_status check_list(int32_t count, const void *a, const void *b) {
-  if (count < 0) return TQ_ERR_SHAPE;
-  if (count > 0 && (!a || !b)) return TQ_ERR_NULL;
+  if (count < 1) return TQ_ERR_SHAPE;
+  if (!a || !b) return TQ_ERR_NULL;
   if (!aligned_to(a, 4) || !aligned_to(b, 4)) return TQ_ERR_ALIGN;
   return TQ_OK;
 }

@@ -866,7 +866,7 @@ extern "C" {
 
 size_t tq_kv4_attention_workspace_bytes(const tq_kv4_cache *c, int32_t count, int32_t tokens, int32_t max_q,
                                         int32_t q_heads) {
-  if (check_cache(c) != TQ_OK || count < 0 || tokens < 0 || max_q < 0 || q_heads < 1 || q_heads % c->heads != 0)
+  if (check_cache(c) != TQ_OK || count < 1 || tokens < 0 || max_q < 0 || q_heads < 1 || q_heads % c->heads != 0)
     return 0;
   return split_ws_bytes(c->dim, split_tiles(max_q, q_heads / c->heads));
 }
@@ -889,7 +889,7 @@ tq_status tq_kv4_attention(const tq_kv4_cache *c, int32_t layer, int32_t count, 
       !aligned_to(d_status, 4))
     return TQ_ERR_ALIGN;
   if (workspace_bytes < tq_kv4_attention_workspace_bytes(c, count, tokens, max_q, q_heads)) return TQ_ERR_SHAPE;
-  if (tokens == 0 || count == 0) return TQ_OK;
+  if (tokens == 0) return TQ_OK;
   const int g = q_heads / c->heads;
   const bool many = call_of_many(tokens, max_q, q_heads, c->heads, c->dim), bf16 = dtype == TQ_BF16;
   const AttnArgs a = {*c,  layer,    count,      tokens, q_heads,  causal != 0, window,

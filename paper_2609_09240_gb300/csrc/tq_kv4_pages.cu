@@ -447,7 +447,7 @@ using namespace tq::kv4;
 extern "C" {
 
 size_t tq_kv4_extend_workspace_bytes(const tq_kv4_cache *c, int32_t count, int32_t tokens) {
-  if (check_cache(c) != TQ_OK || count < 0 || tokens < 0) return 0;
+  if (check_cache(c) != TQ_OK || count < 1 || tokens < 0) return 0;
   return ((size_t)extend_words(c->slots, count, tokens) * 4 + 255) / 256 * 256;
 }
 
@@ -469,7 +469,7 @@ tq_status tq_kv4_extend(const tq_kv4_cache *c, int32_t count, const int32_t *slo
   // at most one copied page per entry
   const int64_t units = (page_bytes_of(*c) + kMoveBytes - 1) / kMoveBytes * c->layers * count;
   const int64_t tok = ((int64_t)tokens + kMoveThreads - 1) / kMoveThreads;
-  const int64_t most = units > tok ? units : tok > 0 ? tok : 1;
+  const int64_t most = units > tok ? units : tok;
   const unsigned grid = (unsigned)(most < kMoveCtas ? most : kMoveCtas);
   return from_cuda(launch_dependent(extend_finish_kernel, dim3(grid), kMoveThreads, st, *c, count, slots, tokens,
                                     (const int32_t *)indptr, where, ws));
@@ -481,7 +481,6 @@ tq_status tq_kv4_fork(const tq_kv4_cache *c, int32_t count, const int32_t *src, 
   if (tq_status s = check_list(count, src, dst)) return s;
   if (!d_status) return TQ_ERR_NULL;
   if (!aligned_to(d_status, 4)) return TQ_ERR_ALIGN;
-  if (count == 0) return TQ_OK;
   return from_cuda(launch_dependent(fork_kernel, dim3((unsigned)count), kListThreads, (cudaStream_t)stream, *c, count,
                                     src, dst, d_status));
 }
@@ -492,7 +491,6 @@ tq_status tq_kv4_free(const tq_kv4_cache *c, int32_t count, const int32_t *slots
   if (tq_status s = check_list(count, slots, slots)) return s;
   if (!d_status) return TQ_ERR_NULL;
   if (!aligned_to(d_status, 4) || !aligned_to(keep, 4)) return TQ_ERR_ALIGN;
-  if (count == 0) return TQ_OK;
   return from_cuda(launch_dependent(free_kernel, dim3((unsigned)count), kListThreads, (cudaStream_t)stream, *c, count,
                                     slots, keep, d_status));
 }
@@ -527,7 +525,6 @@ tq_status tq_kv4_copy_pages(const tq_kv4_cache *from, const tq_kv4_cache *to, in
   if (tq_status s = check_list(count, src_pages, dst_pages)) return s;
   if (!d_status) return TQ_ERR_NULL;
   if (!aligned_to(d_status, 4)) return TQ_ERR_ALIGN;
-  if (count == 0) return TQ_OK;
   const int64_t units = (page_bytes_of(*from) + kMoveBytes - 1) / kMoveBytes * from->layers;
   const unsigned gy = (unsigned)(count < 65535 ? count : 65535);
   const int64_t gx = (kMoveCtas + gy - 1) / gy;
