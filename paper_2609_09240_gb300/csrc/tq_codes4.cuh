@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "tq_decode_ops.cuh"
+
 namespace tq {
 
 // (w & mask) | bits in one instruction: with two constants the compiler would
@@ -35,16 +37,10 @@ __device__ __forceinline__ void zeros(uint32_t zz, __half2 *za, __half2 *zb) {
 
 // D (+)= A B, 16 x 8 x 16, fp16 operands, fp32 sums; and the same onto zeros.
 __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  mm::mma16816(d, a[0], a[1], a[2], a[3], b0, b1);
 }
 __device__ __forceinline__ void mma_f16_first(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+  mm::mma16816_z(d, a[0], a[1], a[2], a[3], b0, b1);
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;

@@ -152,11 +152,9 @@ struct Runs {
   }
 };
 
-constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr int kTop = 9;             // 2^kTop: where a row's and group's largest P is put
 constexpr float kFirst = -3.0e38f;  // the reference of rows that have seen nothing
 constexpr float kMost = 0x1p100f;   // of the sum, whose exponentials follow the first group's power of two
-constexpr float kLn2 = 0.6931471805599453f;
 
 // A partial result: D values of each row, then the logarithms that the values
 // refer to, then the sums.  A warp leaves at most two, of the segment that its

@@ -9,6 +9,9 @@
 namespace tq {
 namespace kv4 {
 
+constexpr float kInf = std::numeric_limits<float>::infinity();
+constexpr float kLn2 = 0.6931471805599453f;
+
 struct AttnArgs {
   tq_kv4_cache c;
   int32_t layer, count, tokens, q_heads, causal, window;
@@ -60,7 +63,7 @@ __device__ __forceinline__ bool goes_to_tiles(const AttnArgs &a, const Sequence 
 // stay): values down to 2^-27 of the largest keep their bits, smaller ones are
 // rounded as subnormal numbers.
 __device__ __forceinline__ int query_exponent(float top) {
-  return top < std::numeric_limits<float>::infinity() ? min(137 - (int)(__float_as_uint(top) >> 23), 126) : 0;
+  return top < kInf ? min(137 - (int)(__float_as_uint(top) >> 23), 126) : 0;
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 // What a row's scores are multiplied by in front of exp2: positive (the query

@@ -7,6 +7,7 @@
 // pass over the counts.  Decisions that need the whole list (which pages, how
 // many) are made by one block; page contents then move in a second launch
 // whose size of work is read on the device.
+#include "tq_codes4.cuh"
 #include "tq_kv4.cuh"
 #include "tq_launch.cuh"
 #include "tq_sm100.cuh"
@@ -436,7 +437,7 @@ __global__ void __launch_bounds__(kMoveThreads)
   }
 }
 
-constexpr int kMoveCtas = 152 * 8;  // eight blocks of 256 threads fill an SM
+inline int move_ctas() { return sm_count() * 8; }  // eight blocks of 256 threads fill an SM
 
 }  // namespace kv4
 }  // namespace tq
@@ -470,7 +471,7 @@ tq_status tq_kv4_extend(const tq_kv4_cache *c, int32_t count, const int32_t *slo
   const int64_t units = (page_bytes_of(*c) + kMoveBytes - 1) / kMoveBytes * c->layers * count;
   const int64_t tok = ((int64_t)tokens + kMoveThreads - 1) / kMoveThreads;
   const int64_t most = units > tok ? units : tok;
-  const unsigned grid = (unsigned)(most < kMoveCtas ? most : kMoveCtas);
+  const unsigned grid = (unsigned)(most < move_ctas() ? most : move_ctas());
   return from_cuda(launch_dependent(extend_finish_kernel, dim3(grid), kMoveThreads, st, *c, count, slots, tokens,
                                     (const int32_t *)indptr, where, ws));
 }
@@ -513,7 +514,7 @@ tq_status tq_kv4_compact(const tq_kv4_cache *c, int32_t *table_out, int32_t *ref
   cudaError_t e =
       launch_dependent(compact_plan_kernel, dim3(1), kPlanThreads, st, *c, refs_out, remap, live, ws);
   if (e != cudaSuccess) return TQ_ERR_CUDA;
-  return from_cuda(launch_dependent(compact_finish_kernel, dim3(kMoveCtas), kMoveThreads, st, *c, table_out,
+  return from_cuda(launch_dependent(compact_finish_kernel, dim3((unsigned)move_ctas()), kMoveThreads, st, *c, table_out,
                                     (const int32_t *)remap, (const int32_t *)ws, d_status));
 }
 
@@ -527,7 +528,7 @@ tq_status tq_kv4_copy_pages(const tq_kv4_cache *from, const tq_kv4_cache *to, in
   if (!aligned_to(d_status, 4)) return TQ_ERR_ALIGN;
   const int64_t units = (page_bytes_of(*from) + kMoveBytes - 1) / kMoveBytes * from->layers;
   const unsigned gy = (unsigned)(count < 65535 ? count : 65535);
-  const int64_t gx = (kMoveCtas + gy - 1) / gy;
+  const int64_t gx = (move_ctas() + gy - 1) / gy;
   return from_cuda(launch_dependent(copy_pages_kernel, dim3((unsigned)(units < gx ? units : gx), gy), kMoveThreads,
                                     (cudaStream_t)stream, *from, *to, count, src_pages, dst_pages, d_status));
 }

@@ -46,9 +46,7 @@ constexpr int kTile = 128;                   // tokens of a K/V tile, rows of a 
 constexpr int kSoftWarps = 8, kDecWarps = 4, kMmaWarp = 12;
 constexpr int kThreads = 16 * 32;  // four warpgroups, for their register counts
 constexpr int kDecThreads = kDecWarps * 32;
-constexpr float kInf = std::numeric_limits<float>::infinity();
 constexpr float kGrow = 8.0f, kUp = 7.0f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 template <int D>
 struct Lay {
@@ -576,8 +574,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
       load(0);
       look_up(1);
       auto put = [&](unsigned char *tile, int k, const uint4 &codes, uint32_t param) {
-        const uint32_t z = (param & 15u) * 0x10001u;
-        const __half2 za = as_half2(z | 0x64006400u), zb = as_half2(z << 4 | 0x54005400u);
+        __half2 za, zb;
+        zeros(param * 0x10001u, &za, &zb);
         const __half2 s = as_half2((param & 0xFFF0u) * 0x10001u);
         unsigned char *dst = tile + (octet[k] * C + 4 * q) * 128 + (lane & 7) * 16;
         *reinterpret_cast<uint4 *>(dst) = decode(codes.x, s, za, zb);
