@@ -551,7 +551,7 @@ typedef struct {
 /* Bytes of a block; 0 if dim is neither 64 nor 128. */
 TQ_API size_t tq_kv4_block_bytes(int32_t dim);
 
-/* Sequence upkeep.  `count` is the length of the (device) lists.
+/* Sequence upkeep.  `count` >= 1 is the length of the (device) lists.
  *
  * tq_kv4_extend makes room for counts[i] >= 0 new tokens at the end of
  * sequence slots[i], before they are written (tq_kv4_append) and attended to:

@@ -3,7 +3,7 @@
 //
 // Eight lanes hold a group of 64 dimensions, eight values each: 16 bytes in,
 // the group's extremes by three shuffles, 4 bytes of codes out.  A value moves 2
-// bytes in and a little over half a byte out (or the reverse): 4600 tokens of 8
+// bytes in and a little over half a byte out (or the reverse): 8060 tokens of 8
 // heads of 128 in and out again 28 us, where the bytes alone take 12; appending is
 // bound by its instructions (about 150 for eight values), reading by its stores.
 #include "tq_codes4.cuh"

@@ -23,7 +23,9 @@
 //     is under 2^-22 of the row's and group's largest is rounded as a subnormal
 //     number).  A P that overflows shows in what is packed, and moves the row's
 //     references: the maximum may fall behind by a factor of 2^7 before the sums
-//     are rescaled.
+//     are rescaled.  That is a choice for time: followed at once, the largest P is a
+//     power of two times s and needs no rounding, which in an earlier form gave an
+//     error of 2.1e-4 (the output's rounding alone) in 80 us, where 2.4e-4 took 74.
 //
 // Work split.  A unit is one page (64 tokens) of one K/V head for one tile of
 // query rows; a sequence's units lie in a row, sequences one after another.
@@ -47,9 +49,10 @@ namespace kv4 {
 
 // Warps of a block (one block per SM) for NT tiles of eight query rows, and the
 // blocks of 64 tokens that each has under way.  One tile leaves the registers
-// for twelve warps: 48 sequences of 1000 to 8000 tokens take 74 us with twelve
-// (two blocks each; 76 when eight with three took 80); two tiles spill with twelve, and
-// a few queries for each of 16 sequences take 18 us with eight and 21 with twelve.
+// for twelve warps: 48 sequences of 1000 to 8000 tokens take 73 us with twelve
+// (two blocks each; an earlier form 76, with eight and three blocks 80); two tiles
+// spill with twelve, and a few queries for each of 16 sequences take 19 us with eight
+// (that form 18, with twelve 21).
 template <int D, int NT>
 struct Shape {
   static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = kWarps * 32;

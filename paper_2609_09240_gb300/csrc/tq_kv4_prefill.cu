@@ -26,10 +26,15 @@
 // that order and O read back from it.
 //
 // Measured (three prompts of 1223 to 1975 tokens, 5500 to 6000 keys, 32 query heads
-// on 8 of 128 dimensions): 357 us, 1050 TFLOP/s.  Of the 2.2 us per 128 keys the
-// MMAs take 0.87 (the scores' at 55 % of their rate: both operands come from
-// shared memory), the rest is the softmax's chain of a tile, which the other tile's
-// MMAs do not cover; without decoding it would be 329 us.
+// on 8 of 128 dimensions): 354 us, 1060 TFLOP/s.  The tensor cores are busy 47 % of the
+// cycles, about 1.0 of the 2.2 us per 128 keys; the rest is the softmax's chain of
+// a tile, which the other tile's MMAs do not cover (without decoding an earlier form
+// took 329 us of 357).
+//
+// Precision.  P is rounded, the sum of a row adds what it was rounded from: the
+// result carries P's rounding (2^-12 on average of what a key brings).  A reference
+// that follows the maximum at once would make the largest P exactly 2^7, at the
+// price of rescaling O at every rise.
 #include <cmath>
 #include <limits>
 
@@ -461,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const AttnArg
         }
         // The scores meet their reference as differences (its product with F would round
         // away what sets scores of ten digits apart), two at a time: as single operations
-        // the subtractions would take 30 us of the pass below.
+        // the subtractions would take 30 us more of the pass above.
         const Pair ref = twice(m == -kInf ? 0.0f : -m), F2 = twice(F), up = twice(kUp);
         Pair s2[2] = {twice(0.0f), twice(0.0f)};
 #pragma unroll

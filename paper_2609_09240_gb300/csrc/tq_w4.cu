@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(256)
 // Split.  A block (one per SM, 16 warps) has a run of whole row tiles, its warps
 // equal runs of their (tile, group) units: a unit is 1088 bytes in a row, which a
 // warp reads straight into registers three units ahead (50 KB under way per
-// SM; four to six ahead change nothing).  One token and 131072 x 4096: 59 us, 4.8
+// SM; four to six ahead change nothing).  One token and 131072 x 4096: 60 us, 4.8
 // TB/s, half of the issue slots busy and the rest waiting for memory.  A tile that
 // several warps share is summed in shared memory in the order
 // of the warps.  Every block holds x in operand order.
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     at += kTile;
   };
   // A request to L2 for the kAhead units after those just asked for (one
-  // instruction, no registers): with it 131072 x 4096 takes 61 us, without 69.
+  // instruction, no registers): with it 131072 x 4096 takes 60 us, without 69.
   auto prefetch = [&](int u) {
     const int n = min(kAhead, u1 - u);
     if (lane == 0 && n > 0)
