@@ -1028,6 +1028,10 @@ class W4Weight:
     """A projection in 4 bits (tq_w4_weight): its tiles on the device."""
 
     def __init__(self, N, K, tiles):
+        n = int(lib().tq_w4_bytes(N, K))
+        if n == 0:
+            raise TQError(-2, "tq_w4_bytes")
+        _want(tiles, "tiles", torch.uint8, (n,))
         self.N, self.K, self.tiles = N, K, tiles
         s = tq_w4_weight(N, K)
         s.tiles = tiles.data_ptr()
